@@ -132,6 +132,53 @@ typedef struct {
     int32_t dz_accumulate;  /* as in cart_attn_desc */
 } cart_attn_varlen_desc;
 
+/* How the 8-bit cache holds a value: a code times the scale of its block of tokens and head.
+ *   CART_E4M3  8-bit floats, sign, 4 exponent and 3 fraction bits, no infinities, up to 448
+ *   CART_I8    integers -127..127 */
+typedef enum { CART_E4M3 = 0, CART_I8 = 1 } cart_cache_format;
+#define CART_CACHE_BLOCK 64
+
+/* One layer's 8-bit key/value cache: a pool of blocks of 64 tokens.  A sequence is a list of block
+ * ids (a row of a block table, or a cart_cache_segment): its token t is row t % 64 of block list[t / 64].
+ * A block id outside [0, n_blocks) means "no block". */
+typedef struct {
+    int32_t n_blocks;       /* >= 1 */
+    int32_t Hkv;            /* key/value heads, >= 1 */
+    int32_t D;              /* head_dim: 64 or 128 (else CART_ERR_UNSUPPORTED) */
+    cart_cache_format format;
+    void *k, *v;            /* [n_blocks,Hkv,64,D] codes, 16-byte aligned */
+    float *k_scale, *v_scale;   /* [n_blocks,Hkv]; every scale > 0 (or NaN, see cart_cache_write), 4-byte aligned */
+} cart_cache;
+
+/* Rows of K and V on their way into or out of a cart_cache. */
+typedef struct {
+    int32_t T;              /* rows of this call, all requests, >= 0 */
+    int32_t B;              /* requests, >= 1 */
+    int32_t max_blocks;     /* row length of the block table, >= 1 */
+    cart_dtype dtype;       /* of the rows: CART_F32 or CART_BF16 */
+    /* element (t, h, d) of k lies at k + t k_row_stride + h k_head_stride + d, likewise of v; strides in
+     * elements, >= 0, whole multiples of 16 bytes ([T,Hkv,D]: Hkv D and D; [Hkv,T,D]: D and T D) */
+    int64_t k_row_stride, k_head_stride, v_row_stride, v_head_stride;
+} cart_cache_rows;
+
+/* Tokens 0 .. p-1 of a sequence that every request of a decode step attends over: a cartridge. */
+typedef struct {
+    const int32_t *blocks;  /* [ceil(p/64)] block ids, device memory */
+    int32_t p;              /* 0 .. 2^30 (an empty segment adds nothing) */
+} cart_cache_segment;
+
+/* Decode step over a cart_cache. */
+typedef struct {
+    int32_t B;              /* requests, >= 1 */
+    int32_t Hq;             /* query heads, a multiple of the cache's Hkv, at most 32 a KV head */
+    int32_t n_shared;       /* 0..CART_MAX_SEGMENTS segments every request attends over */
+    int32_t max_blocks;     /* row length of the block table, >= 0 (0: no request has rows of its own) */
+    int32_t max_own_len;    /* upper bound on any request's own length, 0 .. 64 max_blocks and 2^30 (rows past
+                               a smaller value go unattended) */
+    cart_dtype dtype;       /* of q and o: CART_BF16 */
+    float softmax_scale;    /* 0 selects 1/sqrt(D) */
+} cart_cache_decode_desc;
+
 /* Bytes of workspace each entry point needs for the given descriptor (0 on an invalid one).  The
  * attention and decode figures depend on the number of CUs of the current device as well (work is cut
  * into as many parts as the chip keeps resident): ask with the device current that the call will run
@@ -145,6 +192,8 @@ size_t cart_attn_varlen_bwd_workspace(const cart_attn_varlen_desc *desc);
 size_t cart_kl_workspace(const cart_kl_desc *desc);
 size_t cart_decode_workspace(const cart_decode_desc *desc);
 size_t cart_decode_composed_workspace(const cart_decode_composed_desc *desc, const cart_segment *shared);
+size_t cart_cache_decode_workspace(const cart_cache_decode_desc *desc, const cart_cache *cache,
+                                   const cart_cache_segment *shared);
 
 /*
  * cart_attn_fwd -- Eq. 1 (Sec. 2.3) over the cartridge cache of Sec. 3.2.
@@ -268,6 +317,61 @@ cart_status cart_decode_composed(const cart_decode_composed_desc *desc, const vo
                                  const int32_t *cart_id, const void *k_own, const void *v_own,
                                  const int32_t *cu_lens, void *o, float *lse, void *workspace,
                                  size_t workspace_bytes, void *stream);
+
+/*
+ * cart_cache_write -- rows of K and V into an 8-bit cache.  Rows i of request b (packed rows
+ * cu_rows[b] .. cu_rows[b+1]-1) become tokens first[b] + i of its sequence, row b of `table`.
+ * For every block touched and every head, K and V each by itself, with m the largest magnitude of
+ * the block's new rows and qmax = 127 (CART_I8) or 448 (CART_E4M3):
+ *   scale = the smallest power of two with m <= qmax scale, 2^-64 at least; and where the block held
+ *           rows before (first[b] is not its first token), at least the scale it had;
+ *   code  = x / scale, rounded to the nearest representable value, half to even.
+ * A scale that grows has the codes of the rows before first[b] rounded again (they keep value / new
+ * scale; each growth at least doubles the scale, so all roundings of a value add up to less than
+ * scale (CART_I8), and are exact but for the smallest values (CART_E4M3)).  Rows of the block past
+ * the new ones are left as they are; a block whose first token is among the new rows is begun anew.
+ * A new row with a NaN, an infinity or a magnitude of 2^127 or more makes the scale NaN (the rows of
+ * that block and head read as NaN) until the block is begun anew.
+ *   k, v     rows as cart_cache_rows describes them        in
+ *   cu_rows  [B+1] int32 (device), cu_rows[0] = 0, non-decreasing, cu_rows[B] <= T; NULL: T / B rows each
+ *            (B must divide T)                             in
+ *   first    [B] int32 (device), >= 0; NULL: all 0         in
+ *   table    [B,max_blocks] int32 (device)                 in
+ *   the cache's codes and scales                           in, out
+ * Rows past 64 max_blocks tokens, of a request with a negative `first`, or whose block id is outside
+ * [0, n_blocks) are not written.  No two requests of a call may touch the same block (their codes
+ * and its scale are unspecified then).  No workspace.
+ */
+cart_status cart_cache_write(const cart_cache *cache, const cart_cache_rows *rows, const void *k,
+                             const void *v, const int32_t *cu_rows, const int32_t *first,
+                             const int32_t *table, void *stream);
+
+/*
+ * cart_cache_read -- rows out of an 8-bit cache: code * scale (exact in bf16 and fp32 with the scales
+ * cart_cache_write leaves), tokens first[b] + i of request b's sequence into packed row cu_rows[b] + i.
+ * Arguments as in cart_cache_write, k and v out; requests may share blocks.  Rows without a block
+ * (past the table, an id outside [0, n_blocks), a negative `first`) are written as 0; rows from
+ * cu_rows[B] on are left as they are.
+ */
+cart_status cart_cache_read(const cart_cache *cache, const cart_cache_rows *rows, void *k, void *v,
+                            const int32_t *cu_rows, const int32_t *first, const int32_t *table,
+                            void *stream);
+
+/*
+ * cart_cache_decode -- cart_decode_composed over an 8-bit cache: request b attends over the n_shared
+ * segments of `shared`, then over tokens 0 .. cu_lens[b+1]-cu_lens[b]-1 of its own sequence, row b of
+ * `table` (a private cartridge is the sequence's beginning); all visible.  Tokens without a block (an
+ * id outside [0, n_blocks)) are not attended.  A request without any token has o = 0, lse = -inf.
+ * Codes become bf16 exactly; q and the softmax weights are bf16 operands, sums are fp32.
+ *   q [B,Hq,D] in;  shared: host array of n_shared segments, read during the call only (the block
+ *   lists it points to are read by the kernels);  table [B,max_blocks] int32 in, cu_lens [B+1] int32
+ *   in (device, cu_lens[0] = 0, non-decreasing) -- both may be NULL when max_own_len == 0;
+ *   o [B,Hq,D] out;  lse [B,Hq] fp32 out, may be NULL.
+ */
+cart_status cart_cache_decode(const cart_cache_decode_desc *desc, const cart_cache *cache, const void *q,
+                              const cart_cache_segment *shared, const int32_t *table,
+                              const int32_t *cu_lens, void *o, float *lse, void *workspace,
+                              size_t workspace_bytes, void *stream);
 
 /*
  * cart_attn_varlen_fwd / cart_attn_varlen_bwd -- cart_attn_fwd / cart_attn_bwd (Eq. 1 over the

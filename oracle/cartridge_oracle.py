@@ -362,3 +362,130 @@ def attn_varlen_bwd(q, k_own, v_own, z_k, z_v, d_o, cu_seqlens, scale: Optional[
         d_zk += g[3]
         d_zv += g[4]
     return d_q, d_k, d_v, d_zk, d_zv
+
+
+# ---- the 8-bit key/value cache ------------------------------------------------------------------
+CACHE_BLOCK = 64
+CACHE_QMAX = {"e4m3": 448.0, "i8": 127.0}
+CACHE_MIN_SCALE = 2.0 ** -64
+
+
+def cache_meaning(fmt: str):
+    """What each of the 256 codes stands for: integers in two's complement, or sign, 4 exponent bits (bias 7) and 3 fraction
+    bits without infinities (all ones: NaN)."""
+    x = np.zeros(256)
+    for c in range(256):
+        if fmt == "i8":
+            x[c] = c - 256 if c >= 128 else c
+        else:
+            e, m = (c >> 3) & 15, c & 7
+            x[c] = math.nan if c & 127 == 127 else math.ldexp(8 + m, e - 10) if e else math.ldexp(m, -9)
+            x[c] = -x[c] if c & 128 else x[c]
+    return x
+
+
+def cache_nearest(x, fmt: str):
+    """The codes next to each of x in [-qmax, qmax]; of two as near the one whose last bit is 0."""
+    x = _f64(x)
+    means = cache_meaning(fmt)
+    codes = np.array([c for c in range(256) if abs(means[c]) <= CACHE_QMAX[fmt] and not (means[c] == 0 and c)])   # (no -0)
+    codes = codes[np.argsort(means[codes])]
+    values = means[codes]
+    hi = np.clip(np.searchsorted(values, x), 1, len(values) - 1)
+    below, above = x - values[hi - 1], values[hi] - x
+    up = (above < below) | ((above == below) & (codes[hi] % 2 == 0))
+    return codes[np.where(up, hi, hi - 1)].astype(np.uint8)
+
+
+def cache_scale(amax: float, fmt: str) -> float:
+    """The smallest power of two (2^-64 at least) with amax <= qmax * scale; NaN from magnitudes of 2^127 on."""
+    if not amax < 2.0 ** 127:
+        return math.nan
+    s = CACHE_MIN_SCALE
+    while amax > CACHE_QMAX[fmt] * s:
+        s *= 2.0
+    return s
+
+
+def cache_write(codes, scale, x, table, first, cu_rows, fmt: str):
+    """Rows of K or V into an 8-bit cache, in place.  codes [n_blocks,Hkv,64,d] uint8, scale [n_blocks,Hkv] float64,
+    x [T,Hkv,d]; rows cu_rows[b] .. cu_rows[b+1]-1 become tokens first[b], ... of the sequence in blocks table[b]."""
+    x, means = _f64(x), cache_meaning(fmt)
+    for b in range(len(table)):
+        n, f = int(cu_rows[b + 1] - cu_rows[b]), int(first[b])
+        if f < 0:
+            continue
+        for j in range(f // CACHE_BLOCK, (f + n - 1) // CACHE_BLOCK + 1 if n else 0):
+            lo, hi = max(f, CACHE_BLOCK * j), min(f + n, CACHE_BLOCK * (j + 1))
+            if j >= len(table[b]) or not 0 <= int(table[b][j]) < len(codes):
+                continue
+            blk, kept = int(table[b][j]), lo - CACHE_BLOCK * j
+            rows = x[cu_rows[b] + lo - f:cu_rows[b] + hi - f]
+            for h in range(x.shape[1]):
+                m = np.abs(rows[:, h])
+                s = cache_scale(float(m.max()) if np.isfinite(m).all() else math.inf, fmt)
+                old = float(scale[blk, h])
+                if kept:
+                    s = max(s, old) if not (math.isnan(s) or math.isnan(old)) else math.nan
+                scale[blk, h] = s
+                if math.isnan(s):
+                    continue                    # the codes mean nothing any more
+                if kept and s > old:
+                    codes[blk, h, :kept] = cache_nearest(means[codes[blk, h, :kept]] * (old / s), fmt)
+                codes[blk, h, kept:kept + len(rows)] = cache_nearest(rows[:, h] / s, fmt)
+
+
+def cache_history(codes, scale, blocks, n: int, fmt: str):
+    """Tokens 0 .. n-1 of the sequence in `blocks` -> [n,Hkv,d] and which of them exist [n]."""
+    means = cache_meaning(fmt)
+    x = np.zeros((n,) + (codes.shape[1], codes.shape[3]))
+    there = np.zeros(n, dtype=bool)
+    for j in range(-(-n // CACHE_BLOCK)):
+        if j >= len(blocks) or not 0 <= int(blocks[j]) < len(codes):
+            continue
+        lo, hi, blk = CACHE_BLOCK * j, min(n, CACHE_BLOCK * (j + 1)), int(blocks[j])
+        x[lo:hi] = (means[codes[blk, :, :hi - lo]] * _f64(scale[blk])[:, None, None]).transpose(1, 0, 2)
+        there[lo:hi] = True
+    return x, there
+
+
+def cache_read(codes, scale, table, first, cu_rows, fmt: str):
+    """The rows that cache_write would fill, out of the cache: [T,Hkv,d]; 0 where there is no block."""
+    out = np.zeros((int(cu_rows[len(table)]),) + (codes.shape[1], codes.shape[3]))
+    for b in range(len(table)):
+        f, n = int(first[b]), int(cu_rows[b + 1] - cu_rows[b])
+        if f >= 0 and n:
+            x, there = cache_history(codes, scale, table[b], f + n, fmt)
+            out[cu_rows[b]:cu_rows[b + 1]] = np.where(there[:, None, None], x, 0.0)[f:]
+    return out
+
+
+def cache_decode(q, k, k_scale, v, v_scale, shared, table, cu_lens, fmt: str, scale: Optional[float] = None):
+    """Decode step over an 8-bit cache: request b attends over tokens 0 .. p-1 of every (blocks, p) of `shared`, then over
+    tokens 0 .. cu_lens[b+1]-cu_lens[b]-1 of its own blocks table[b]; all visible, tokens without a block left out, a
+    request without any has o = 0, lse = -inf.
+    Returns o [B,Hq,d], lse [B,Hq], and what the error of each is measured by: the weighted sum of |v| [B,Hq,d] and the
+    largest scale * sum_d |q_d k_d| [B,Hq] over the keys."""
+    q = _f64(q)
+    B, Hq, d = q.shape
+    G = Hq // k.shape[1]
+    if scale is None:
+        scale = 1.0 / math.sqrt(d)
+    pick = lambda blocks, n: [x[there] for x, there in (cache_history(k, k_scale, blocks, n, fmt), cache_history(v, v_scale, blocks, n, fmt))]
+    common = [pick(blocks, p) for blocks, p in shared]
+    o, lse, size, reach = np.zeros((B, Hq, d)), np.full((B, Hq), -math.inf), np.zeros((B, Hq, d)), np.zeros((B, Hq))
+    for b in range(B):
+        parts = common + ([pick(table[b], int(cu_lens[b + 1] - cu_lens[b]))] if table is not None else [])
+        keys = np.concatenate([np.zeros((0,) + k.shape[1::2])] + [p[0] for p in parts])
+        vals = np.concatenate([np.zeros((0,) + k.shape[1::2])] + [p[1] for p in parts])
+        if not len(keys):
+            continue
+        for h in range(Hq):
+            s = scale * (keys[:, h // G] @ q[b, h])
+            m = s.max()
+            e = np.exp(s - m)
+            o[b, h] = (e / e.sum()) @ vals[:, h // G]
+            size[b, h] = (e / e.sum()) @ np.abs(vals[:, h // G])
+            lse[b, h] = m + math.log(e.sum())
+            reach[b, h] = scale * (np.abs(keys[:, h // G]) @ np.abs(q[b, h])).max()
+    return o, lse, size, reach

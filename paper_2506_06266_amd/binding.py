@@ -10,7 +10,7 @@ from __future__ import annotations
 import ctypes as C
 import importlib.util
 import os
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 
@@ -27,7 +27,8 @@ EXPORTS = ["cart_attn_fwd_workspace", "cart_attn_bwd_workspace", "cart_kl_worksp
            "cart_decode", "cart_decode_composed_workspace", "cart_decode_composed", "cart_teacher_topk",
            "cart_attn_varlen_fwd_workspace", "cart_attn_varlen_bwd_workspace", "cart_attn_varlen_fwd",
            "cart_attn_varlen_bwd", "cart_trace_events", "cart_calib_mfma", "cart_calib_copy",
-           "cart_calib_read", "cart_decode_static", "cart_decode_static_capacity",
+           "cart_calib_read", "cart_cache_write", "cart_cache_read", "cart_cache_decode",
+           "cart_cache_decode_workspace", "cart_decode_static", "cart_decode_static_capacity",
            "cart_status_str", "cart_version"]
 
 
@@ -67,6 +68,26 @@ class DecodeDesc(C.Structure):
     _fields_ = [("B", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32),
                 ("P", C.c_int32), ("total_own_tokens", C.c_int32), ("max_own_len", C.c_int32),
                 ("dtype", C.c_int), ("softmax_scale", C.c_float), ("impl", C.c_int)]
+
+
+class CacheStruct(C.Structure):
+    _fields_ = [("n_blocks", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32), ("format", C.c_int), ("k", C.c_void_p),
+                ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+class CacheRows(C.Structure):
+    _fields_ = [("T", C.c_int32), ("B", C.c_int32), ("max_blocks", C.c_int32), ("dtype", C.c_int),
+                ("k_row_stride", C.c_int64), ("k_head_stride", C.c_int64), ("v_row_stride", C.c_int64),
+                ("v_head_stride", C.c_int64)]
+
+
+class CacheSegment(C.Structure):
+    _fields_ = [("blocks", C.c_void_p), ("p", C.c_int32)]
+
+
+class CacheDecodeDesc(C.Structure):
+    _fields_ = [("B", C.c_int32), ("Hq", C.c_int32), ("n_shared", C.c_int32), ("max_blocks", C.c_int32),
+                ("max_own_len", C.c_int32), ("dtype", C.c_int), ("softmax_scale", C.c_float)]
 
 
 class CartridgeError(RuntimeError):
@@ -128,6 +149,13 @@ def load() -> C.CDLL:
     lib.cart_decode_composed_workspace.argtypes = [C.POINTER(DecodeComposedDesc), C.POINTER(Segment)]
     lib.cart_decode_composed.restype = C.c_int
     lib.cart_decode_composed.argtypes = [C.POINTER(DecodeComposedDesc), vp, C.POINTER(Segment)] + [vp] * 9 + [sz, vp]
+    for name in ("cart_cache_write", "cart_cache_read"):
+        f = getattr(lib, name)
+        f.restype, f.argtypes = C.c_int, [C.POINTER(CacheStruct), C.POINTER(CacheRows)] + [vp] * 6
+    lib.cart_cache_decode_workspace.restype = sz
+    lib.cart_cache_decode_workspace.argtypes = [C.POINTER(CacheDecodeDesc), C.POINTER(CacheStruct), C.POINTER(CacheSegment)]
+    lib.cart_cache_decode.restype = C.c_int
+    lib.cart_cache_decode.argtypes = [C.POINTER(CacheDecodeDesc), C.POINTER(CacheStruct), vp, C.POINTER(CacheSegment)] + [vp] * 5 + [sz, vp]
     lib.cart_trace_events.restype = C.c_int
     lib.cart_trace_events.argtypes = [C.POINTER(C.c_void_p), C.c_int32]
     lib.cart_calib_mfma.restype = C.c_double
@@ -316,6 +344,53 @@ def cart_decode_composed(q, shared, pool_k, pool_v, cart_id, k_own, v_own, cu_le
     segs = [(zk, zv) for zk, zv in shared] if len(shared) else []
     return _outputs(_native.decode_composed(q, segs, pool_k, pool_v, cart_id, k_own, v_own, cu_lens, max_own_len, scale, o, lse,
                                             workspace, stream), "cart_decode_composed")
+
+
+# ------------------------------------------------------------------------------------------------
+CACHE_BLOCK = 64
+
+
+class Cache(NamedTuple):
+    """One layer's 8-bit key/value cache: codes k, v [n_blocks,Hkv,64,D] (torch.float8_e4m3fn or torch.int8) and their
+    scales [n_blocks,Hkv] fp32.  (Any four such tensors will do where a cache is taken.)"""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+
+def cache_empty(n_blocks: int, n_kv_heads: int, head_dim: int = 128, dtype=torch.float8_e4m3fn, device="cuda") -> Cache:
+    """A cache without contents; blocks are begun by writing their first token."""
+    codes = lambda: torch.empty(n_blocks, n_kv_heads, CACHE_BLOCK, head_dim, dtype=dtype, device=device)
+    scales = lambda: torch.empty(n_blocks, n_kv_heads, dtype=torch.float32, device=device)
+    return Cache(codes(), codes(), scales(), scales())
+
+
+def cart_cache_write(cache, k, v, table, *, first=None, cu_rows=None, stream=None) -> None:
+    """k, v [T,Hkv,D] (bf16 or fp32, any strides of whole 16 bytes, the last dimension contiguous) become tokens first[b],
+    first[b] + 1, ... of request b, whose blocks are table[b] (int32 [B,max_blocks]); first [B] int32 (None: all 0);
+    cu_rows [B+1] int32 (None: T / B rows of each request)."""
+    load()
+    _outputs(_native.cache_write(cache, k, v, table, first, cu_rows, stream), "cart_cache_write")
+
+
+def cart_cache_read(cache, k, v, table, *, first=None, cu_rows=None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The other way: fills k, v and returns them.  (z_k, z_v [Hkv,P,D] of cart_attn_fwd: z_k.transpose(0, 1),
+    z_v.transpose(0, 1).)"""
+    load()
+    return _outputs(_native.cache_read(cache, k, v, table, first, cu_rows, stream), "cart_cache_read")
+
+
+def cart_cache_decode(q, cache, shared, table, cu_lens, max_own_len: int, *, scale: float = 0.0, o=None, lse=None,
+                      workspace=None, stream=None):
+    """q [B,Hq,D]; shared: list of (blocks int32 [>= ceil(p/64)], p) every request attends over; table [B,max_blocks] and
+    cu_lens [B+1] int32 (device; or None, with max_own_len = 0): the requests' own tokens -> (o [B,Hq,D], lse [B,Hq])."""
+    load()
+    if stream is not None:          # what the call allocates belongs to the stream it is used on
+        with torch.cuda.stream(stream):
+            return cart_cache_decode(q, cache, shared, table, cu_lens, max_own_len, scale=scale, o=o, lse=lse, workspace=workspace)
+    return _outputs(_native.cache_decode(q, cache, shared, table, cu_lens, max_own_len, scale, o, lse, workspace, None),
+                    "cart_cache_decode")
 
 
 # ------------------------------------------------------------------------------------------------

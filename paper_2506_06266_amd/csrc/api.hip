@@ -94,6 +94,61 @@ inline bool use_mfma(const cart_decode_desc& d) {
     return d.impl != CART_IMPL_VECTOR && cart::decode_mfma_supported(d);
 }
 
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// (pointers: only where a kernel will follow them)
+cart_status check_cache(const cart_cache* c, bool pointers) {
+    if (!c) return CART_ERR_NULL;
+    if (c->n_blocks < 1 || c->Hkv < 1 || c->D < 1) return CART_ERR_SHAPE;
+    if (c->D != 64 && c->D != 128) return CART_ERR_UNSUPPORTED;
+    if (c->format != CART_E4M3 && c->format != CART_I8) return CART_ERR_UNSUPPORTED;
+    if (static_cast<double>(c->n_blocks) * c->Hkv * CART_CACHE_BLOCK * c->D > 1099511627776.0) return CART_ERR_SHAPE;
+    if (!pointers) return CART_OK;
+    if (!c->k || !c->v || !c->k_scale || !c->v_scale) return CART_ERR_NULL;
+    if (!aligned16(c->k) || !aligned16(c->v) || !aligned4(c->k_scale) || !aligned4(c->v_scale)) return CART_ERR_ALIGN;
+    return CART_OK;
+}
+
+cart_status check_cache_rows(const cart_cache* c, const cart_cache_rows* r, const void* k, const void* v, const int32_t* cu,
+                             const int32_t* first, const int32_t* table) {
+    if (!r) return CART_ERR_NULL;
+    cart_status s = check_cache(c, true);
+    if (s != CART_OK) return s;
+    if (r->T < 0 || r->B < 1 || r->max_blocks < 1) return CART_ERR_SHAPE;
+    if (r->dtype != CART_F32 && r->dtype != CART_BF16) return CART_ERR_UNSUPPORTED;
+    if (!cu && r->T % r->B != 0) return CART_ERR_SHAPE;
+    const int64_t strides[4] = {r->k_row_stride, r->k_head_stride, r->v_row_stride, r->v_head_stride};
+    for (int64_t x : strides) {
+        if (x < 0 || x > (INT64_C(1) << 40)) return CART_ERR_SHAPE;
+        if (x % (r->dtype == CART_F32 ? 4 : 8) != 0) return CART_ERR_ALIGN;
+    }
+    if (r->T == 0) return CART_OK;
+    if (!k || !v || !table) return CART_ERR_NULL;
+    if (!aligned16(k) || !aligned16(v) || !aligned4(cu) || !aligned4(first) || !aligned4(table)) return CART_ERR_ALIGN;
+    return CART_OK;
+}
+
+cart_status check_cache_decode(const cart_cache_decode_desc* d, const cart_cache* c, const cart_cache_segment* shared, bool pointers) {
+    if (!d) return CART_ERR_NULL;
+    cart_status s = check_cache(c, pointers);
+    if (s != CART_OK) return s;
+    if (d->B < 1 || d->Hq < 1 || d->Hq % c->Hkv != 0) return CART_ERR_SHAPE;
+    if (d->dtype != CART_BF16 || d->Hq / c->Hkv > 32) return CART_ERR_UNSUPPORTED;
+    if (d->n_shared < 0 || d->n_shared > CART_MAX_SEGMENTS) return CART_ERR_SHAPE;
+    if (d->max_blocks < 0 || d->max_own_len < 0 || d->max_own_len > (1 << 30) ||
+        d->max_own_len > static_cast<int64_t>(d->max_blocks) * CART_CACHE_BLOCK)
+        return CART_ERR_SHAPE;
+    if (static_cast<double>(d->B) * d->Hq * c->D > 1099511627776.0) return CART_ERR_SHAPE;
+    if (!(d->softmax_scale >= 0.f) || isinf(d->softmax_scale)) return CART_ERR_SHAPE;
+    if (d->n_shared > 0 && !shared) return CART_ERR_NULL;
+    for (int i = 0; i < d->n_shared; ++i) {
+        if (shared[i].p < 0 || shared[i].p > (1 << 30)) return CART_ERR_SHAPE;
+        if (shared[i].p > 0 && !shared[i].blocks) return CART_ERR_NULL;
+        if (!aligned4(shared[i].blocks)) return CART_ERR_ALIGN;
+    }
+    return CART_OK;
+}
+
 #define REQUIRE(p) do { if (!(p)) return CART_ERR_NULL; } while (0)
 #define ALIGNED(p) do { if (!aligned16(p)) return CART_ERR_ALIGN; } while (0)
 
@@ -320,6 +375,44 @@ cart_status cart_decode_static(const cart_decode_desc* d, const void* q, const v
     const float scale = attn_scale(d->softmax_scale, d->D);
     int e = cart::launch_decode_mfma(*d, scale, q, z_k, z_v, k_own, v_own, cu_lens, o, lse, ws,
                                      static_cast<hipStream_t>(stream));
+    return e == 0 ? CART_OK : CART_ERR_LAUNCH;
+}
+
+cart_status cart_cache_write(const cart_cache* c, const cart_cache_rows* r, const void* k, const void* v, const int32_t* cu_rows,
+                             const int32_t* first, const int32_t* table, void* stream) {
+    cart_status s = check_cache_rows(c, r, k, v, cu_rows, first, table);
+    if (s != CART_OK || r->T == 0) return s;
+    int e = cart::launch_cache_rows(*c, *r, const_cast<void*>(k), const_cast<void*>(v), cu_rows, first, table, true,
+                                    static_cast<hipStream_t>(stream));
+    return e == 0 ? CART_OK : CART_ERR_LAUNCH;
+}
+
+cart_status cart_cache_read(const cart_cache* c, const cart_cache_rows* r, void* k, void* v, const int32_t* cu_rows,
+                            const int32_t* first, const int32_t* table, void* stream) {
+    cart_status s = check_cache_rows(c, r, k, v, cu_rows, first, table);
+    if (s != CART_OK || r->T == 0) return s;
+    int e = cart::launch_cache_rows(*c, *r, k, v, cu_rows, first, table, false, static_cast<hipStream_t>(stream));
+    return e == 0 ? CART_OK : CART_ERR_LAUNCH;
+}
+
+size_t cart_cache_decode_workspace(const cart_cache_decode_desc* d, const cart_cache* c, const cart_cache_segment* shared) {
+    if (check_cache_decode(d, c, shared, false) != CART_OK) return 0;
+    return cart::cache_decode_workspace(*d, *c, shared);
+}
+
+cart_status cart_cache_decode(const cart_cache_decode_desc* d, const cart_cache* c, const void* q, const cart_cache_segment* shared,
+                              const int32_t* table, const int32_t* cu_lens, void* o, float* lse, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+    cart_status s = check_cache_decode(d, c, shared, true);
+    if (s != CART_OK) return s;
+    REQUIRE(q); REQUIRE(o);
+    if (d->max_own_len > 0) { REQUIRE(table); REQUIRE(cu_lens); }
+    ALIGNED(q); ALIGNED(o); ALIGNED(workspace);
+    if (!aligned4(table) || !aligned4(cu_lens) || !aligned4(lse)) return CART_ERR_ALIGN;
+    const size_t need = cart::cache_decode_workspace(*d, *c, shared);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return CART_ERR_WORKSPACE;
+    int e = cart::launch_cache_decode(*d, *c, attn_scale(d->softmax_scale, c->D), q, shared, table, cu_lens, o, lse, workspace,
+                                      static_cast<hipStream_t>(stream));
     return e == 0 ? CART_OK : CART_ERR_LAUNCH;
 }
 

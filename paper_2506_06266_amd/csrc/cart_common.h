@@ -135,4 +135,12 @@ int launch_decode_mfma(const cart_decode_desc& d, float scale, const void* q, co
                        const void* zv, const void* k, const void* v, const int32_t* cu, void* o,
                        float* lse, void* ws, hipStream_t st);
 
+// the 8-bit cache
+int launch_cache_rows(const cart_cache& c, const cart_cache_rows& r, void* k, void* v, const int32_t* cu, const int32_t* first,
+                      const int32_t* table, bool write, hipStream_t st);
+size_t cache_decode_workspace(const cart_cache_decode_desc& d, const cart_cache& c, const cart_cache_segment* shared);
+int launch_cache_decode(const cart_cache_decode_desc& d, const cart_cache& c, float scale, const void* q,
+                        const cart_cache_segment* shared, const int32_t* table, const int32_t* cu, void* o, float* lse, void* ws,
+                        hipStream_t st);
+
 }  // namespace cart

@@ -17,6 +17,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/core/Tensor.h>
+#include <c10/core/DeviceGuard.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
 
@@ -36,6 +37,10 @@ struct Api {
     decltype(&cart_decode) decode;
     decltype(&cart_decode_composed_workspace) composed_workspace;
     decltype(&cart_decode_composed) composed;
+    decltype(&cart_cache_write) cache_write;
+    decltype(&cart_cache_read) cache_read;
+    decltype(&cart_cache_decode_workspace) cache_decode_workspace;
+    decltype(&cart_cache_decode) cache_decode;
 } api;
 
 // a tensor argument (null: None)
@@ -305,6 +310,135 @@ PyObject* decode_composed(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// The tensors of an 8-bit cache, (k, v, k_scale, v_scale): one format, sizes that agree.  `at`: the four, for place().
+cart_cache cache_of(PyObject* o, const at::Tensor** at) {
+    if ((!PyList_Check(o) && !PyTuple_Check(o)) || PySequence_Fast_GET_SIZE(o) != 4) throw torch::TypeError("a cache (k, v, k_scale, v_scale) is expected");
+    const at::Tensor &k = tensor(PySequence_Fast_GET_ITEM(o, 0)), &v = tensor(PySequence_Fast_GET_ITEM(o, 1)),
+                     &ks = tensor(PySequence_Fast_GET_ITEM(o, 2)), &vs = tensor(PySequence_Fast_GET_ITEM(o, 3));
+    cart_cache c = {};
+    if (k.scalar_type() == at::kChar) c.format = CART_I8;
+    else if (k.scalar_type() == at::kFloat8_e4m3fn) c.format = CART_E4M3;
+    else throw torch::TypeError(std::string("unsupported dtype ") + c10::toString(k.scalar_type()));
+    c.n_blocks = size(k, 4, 0); c.Hkv = size(k, 4, 1); c.D = size(k, 4, 3);
+    TORCH_CHECK_VALUE(k.size(2) == CART_CACHE_BLOCK, "blocks of ", k.size(2), " tokens where ", CART_CACHE_BLOCK, " are expected");
+    TORCH_CHECK_VALUE(v.scalar_type() == k.scalar_type() && v.sizes() == k.sizes(), "k and v of a cache differ in dtype or sizes");
+    for (const at::Tensor* t : {&ks, &vs})
+        TORCH_CHECK_VALUE(t->scalar_type() == at::kFloat && t->dim() == 2 && t->size(0) == c.n_blocks && t->size(1) == c.Hkv,
+                          "the scales of a cache are fp32 [n_blocks, Hkv]");
+    at[0] = &k; at[1] = &v; at[2] = &ks; at[3] = &vs;
+    return c;
+}
+// their addresses, on one device
+void place(cart_cache& c, const at::Tensor* const* at) {
+    c.k = address(at[0]); c.v = address(at[1]);
+    c.k_scale = static_cast<float*>(address(at[2])); c.v_scale = static_cast<float*>(address(at[3]));
+    for (int i = 1; i < 4; ++i) TORCH_CHECK_VALUE(at[i]->device() == at[0]->device(), "the tensors of a cache are on different devices");
+}
+// an int32 array of `n` values (-1: any number)
+const at::Tensor* indices(const at::Tensor* t, int64_t n, const char* what) {
+    if (!t) return nullptr;
+    if (t->scalar_type() != at::kInt) throw torch::TypeError(std::string(what) + " is an int32 tensor");
+    TORCH_CHECK_VALUE(n < 0 || t->numel() == n, what, " has ", t->numel(), " values where ", n, " are expected");
+    return t;
+}
+// its address, and of anything else that has to be on the cache's device
+template <typename T>
+T* beside(const at::Tensor* t, const at::Tensor& codes) {
+    void* const p = address(t);
+    TORCH_CHECK_VALUE(!t || t->device() == codes.device(), "a tensor is on another device than the cache");
+    return static_cast<T*>(p);
+}
+
+// cache, k, v, table, first, cu_rows, stream
+PyObject* cache_rows(PyObject* const* a, Py_ssize_t n, bool write) {
+    count(n, 7);
+    const at::Tensor* at[4];
+    cart_cache c = cache_of(a[0], at);
+    const at::Tensor &k = tensor(a[1]), &v = tensor(a[2]), &table = tensor(a[3]);
+    cart_cache_rows r = {};
+    r.dtype = static_cast<decltype(r.dtype)>(dtype_code(k));
+    r.T = size(k, 3, 0);
+    r.B = size(table, 2, 0); r.max_blocks = size(table, 2, 1);
+    TORCH_CHECK_VALUE(k.size(1) == c.Hkv && k.size(2) == c.D, "rows of ", k.size(1), " heads of ", k.size(2), " beside a cache of ", c.Hkv, " of ", c.D);
+    TORCH_CHECK_VALUE(v.scalar_type() == k.scalar_type() && v.sizes() == k.sizes(), "k and v differ in dtype or sizes");
+    const at::Tensor *pt = indices(&table, -1, "table"), *pf = indices(tensor_or_none(a[4]), r.B, "first"),
+                     *pc = indices(tensor_or_none(a[5]), static_cast<int64_t>(r.B) + 1, "cu_rows");
+    place(c, at);
+    void* p[2];
+    int64_t* const strides[2][2] = {{&r.k_row_stride, &r.k_head_stride}, {&r.v_row_stride, &r.v_head_stride}};
+    for (int i = 0; i < 2; ++i) {
+        const at::Tensor& t = i ? v : k;
+        TORCH_CHECK_VALUE(t.is_cuda() && t.device() == at[0]->device() && t.stride(2) == 1,
+                          "rows handed to libcartridge must be device tensors beside the cache, their last dimension contiguous");
+        p[i] = t.mutable_data_ptr();
+        *strides[i][0] = t.size(0) > 1 ? t.stride(0) : 0;
+        *strides[i][1] = t.size(1) > 1 ? t.stride(1) : 0;
+    }
+    const int32_t *it = beside<int32_t>(pt, *at[0]), *jf = beside<int32_t>(pf, *at[0]), *jc = beside<int32_t>(pc, *at[0]);
+    const c10::DeviceGuard on(at[0]->device());
+    void* const st = stream(a[6]);
+    const int status = without_gil([&] {
+        return write ? api.cache_write(&c, &r, p[0], p[1], jc, jf, it, st) : api.cache_read(&c, &r, p[0], p[1], jc, jf, it, st);
+    });
+    return outputs(status, {&k, &v});
+}
+PyObject* cache_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    return cache_rows(a, n, true);
+    END_HANDLE_TH_ERRORS
+}
+PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    return cache_rows(a, n, false);
+    END_HANDLE_TH_ERRORS
+}
+
+// q, cache, shared (a list of pairs), table, cu_lens, max_own_len, scale, o, lse, workspace, stream
+PyObject* cache_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    count(n, 11);
+    const at::Tensor& q = tensor(a[0]);
+    cart_cache_decode_desc d = {};
+    d.B = size(q, 3, 0); d.Hq = size(q, 3, 1);
+    d.dtype = static_cast<decltype(d.dtype)>(dtype_code(q));
+    const at::Tensor* at[4];
+    cart_cache c = cache_of(a[1], at);
+    TORCH_CHECK_VALUE(q.size(2) == c.D, "queries of ", q.size(2), " dimensions beside a cache of ", c.D);
+    if (!PyList_Check(a[2]) && !PyTuple_Check(a[2])) throw torch::TypeError("a list of (blocks, p) is expected");
+    d.n_shared = static_cast<int32_t>(PySequence_Fast_GET_SIZE(a[2]));
+    std::vector<cart_cache_segment> segs(static_cast<size_t>(std::max(d.n_shared, 1)));
+    auto blocks_of = [&](int32_t i) -> const at::Tensor& { return tensor(PySequence_Fast_GET_ITEM(PySequence_Fast_GET_ITEM(a[2], i), 0)); };
+    for (int32_t i = 0; i < d.n_shared; ++i) {
+        PyObject* const pair = PySequence_Fast_GET_ITEM(a[2], i);
+        if ((!PyList_Check(pair) && !PyTuple_Check(pair)) || PySequence_Fast_GET_SIZE(pair) != 2) throw torch::TypeError("a pair (blocks, p) is expected");
+        const at::Tensor& blocks = *indices(&blocks_of(i), -1, "the blocks of a segment");
+        segs[i].p = int32(PySequence_Fast_GET_ITEM(pair, 1));
+        TORCH_CHECK_VALUE(blocks.numel() * CART_CACHE_BLOCK >= segs[i].p, "a segment of ", segs[i].p, " tokens in ", blocks.numel(), " blocks");
+    }
+    const at::Tensor *table = indices(tensor_or_none(a[3]), -1, "table"), *cu = indices(tensor_or_none(a[4]), static_cast<int64_t>(d.B) + 1, "cu_lens");
+    if (table) {
+        TORCH_CHECK_VALUE(size(*table, 2, 0) == d.B, "a table of ", table->size(0), " requests where ", d.B, " are expected");
+        d.max_blocks = size(*table, 2, 1);
+    }
+    d.max_own_len = int32(a[5]);
+    d.softmax_scale = real(a[6]);
+    place(c, at);
+    void* const pq = beside<void>(&q, *at[0]);
+    for (int32_t i = 0; i < d.n_shared; ++i) segs[i].blocks = beside<int32_t>(&blocks_of(i), *at[0]);
+    const int32_t *pt = beside<int32_t>(table, *at[0]), *pc = beside<int32_t>(cu, *at[0]);
+    const at::Tensor o = like(a[7], q), lse = fresh(a[8], {d.B, d.Hq}, at::kFloat, q);
+    TORCH_CHECK_VALUE(o.scalar_type() == q.scalar_type() && o.numel() == q.numel(), "o differs from q in dtype or size");
+    TORCH_CHECK_VALUE(lse.scalar_type() == at::kFloat && lse.numel() == static_cast<int64_t>(d.B) * d.Hq, "lse is fp32 [B, Hq]");
+    void *po = beside<void>(&o, *at[0]), *pl = beside<void>(&lse, *at[0]);
+    const c10::DeviceGuard on(at[0]->device());
+    const Workspace ws(a[9], api.cache_decode_workspace(&d, &c, segs.data()), q);
+    void* const st = stream(a[10]);
+    return outputs(without_gil([&] {
+        return api.cache_decode(&d, &c, pq, segs.data(), pt, pc, po, static_cast<float*>(pl), ws.p, ws.bytes, st);
+    }), {&o, &lse});
+    END_HANDLE_TH_ERRORS
+}
+
 // the handle of the opened library, the binding's _stream
 PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
@@ -328,13 +462,17 @@ PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
     get(api.decode, "cart_decode");
     get(api.composed_workspace, "cart_decode_composed_workspace");
     get(api.composed, "cart_decode_composed");
+    get(api.cache_write, "cart_cache_write");
+    get(api.cache_read, "cart_cache_read");
+    get(api.cache_decode_workspace, "cart_cache_decode_workspace");
+    get(api.cache_decode, "cart_cache_decode");
     Py_RETURN_NONE;
     END_HANDLE_TH_ERRORS
 }
 
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(attn_fwd), FAST(attn_bwd), FAST(distill_kl), FAST(teacher_topk), FAST(decode), FAST(decode_composed),
-                         FAST(init), {nullptr, nullptr, 0, nullptr}};
+                         FAST(cache_write), FAST(cache_read), FAST(cache_decode), FAST(init), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
