@@ -184,7 +184,8 @@ typedef struct {
  * into as many parts as the chip keeps resident): ask with the device current that the call will run
  * on.  An attention workspace also serves every call of the same heads, dtype and layout none of whose
  * sizes (B, S, P; T, B, max_seqlen, P) is larger: one sized for a program's largest batch can be kept.  So
- * does a decode workspace of up to 32 MiB (B, T, max_own_len, segments and pool_p). */
+ * does a decode workspace of up to 32 MiB (B, T, max_own_len, segments and pool_p), and a cache decode workspace
+ * of any size (B, max_own_len, segments). */
 size_t cart_attn_fwd_workspace(const cart_attn_desc *desc);
 size_t cart_attn_bwd_workspace(const cart_attn_desc *desc);
 size_t cart_attn_varlen_fwd_workspace(const cart_attn_varlen_desc *desc);
@@ -361,7 +362,8 @@ cart_status cart_cache_read(const cart_cache *cache, const cart_cache_rows *rows
  * cart_cache_decode -- cart_decode_composed over an 8-bit cache: request b attends over the n_shared
  * segments of `shared`, then over tokens 0 .. cu_lens[b+1]-cu_lens[b]-1 of its own sequence, row b of
  * `table` (a private cartridge is the sequence's beginning); all visible.  Tokens without a block (an
- * id outside [0, n_blocks)) are not attended.  A request without any token has o = 0, lse = -inf.
+ * id outside [0, n_blocks)) are not attended.  A request without any token has o = 0, lse = -inf;
+ * a scale of NaN makes o and lse of the heads that attend to its block NaN.
  * Codes become bf16 exactly; q and the softmax weights are bf16 operands, sums are fp32.
  *   q [B,Hq,D] in;  shared: host array of n_shared segments, read during the call only (the block
  *   lists it points to are read by the kernels);  table [B,max_blocks] int32 in, cu_lens [B+1] int32
