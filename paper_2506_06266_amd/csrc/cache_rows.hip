@@ -10,6 +10,21 @@ using namespace cache;
 
 namespace {
 
+// Rows of a call past what the memory-side cache keeps of them are moved non-temporally (NT), so that the codes stay in it.  us a call:
+// writing 64 prompts (150 MB of rows) 48.2, so 40.7; 537 MB 153.8, 155.0; a cartridge of 67 MB 17.3, 20.3; reading back 537 MB
+// 160.8, 155.7, a cartridge of 34 MB 10.4, 10.1 (and whoever reads it next would find less of it).
+constexpr long NT_BYTES = 100000000;
+template <bool NT, typename V> __device__ __forceinline__ V load_as(const char* p) {
+    const V* const q = reinterpret_cast<const V*>(p);
+    if constexpr (NT) return __builtin_nontemporal_load(q);
+    else return *q;
+}
+template <bool NT, typename V> __device__ __forceinline__ void store_as(char* p, V v) {
+    V* const q = reinterpret_cast<V*>(p);
+    if constexpr (NT) __builtin_nontemporal_store(v, q);
+    else *q = v;
+}
+
 struct RowsArgs {
     const int32_t *cu, *first, *table;
     int T, B, max_blocks, n_blocks, Hkv;
@@ -58,27 +73,27 @@ __device__ __forceinline__ Piece piece_of(const RowsArgs& a, int place, int lane
 }
 
 // 8 elements of a row as fp32 bits or values
-template <typename T> struct Eight;
-template <> struct Eight<float> {
+template <typename T, bool NT> struct Eight;
+template <bool NT> struct Eight<float, NT> {
     u32x4 a, b;
     __device__ __forceinline__ void load(const char* p) {
-        a = *reinterpret_cast<const u32x4*>(p);
-        b = *reinterpret_cast<const u32x4*>(p + 16);
+        a = load_as<NT, u32x4>(p);
+        b = load_as<NT, u32x4>(p + 16);
     }
     __device__ __forceinline__ uint32_t bits(int i) const { return i < 4 ? a[i] : b[i - 4]; }
     static __device__ __forceinline__ void store(char* p, const float (&x)[8]) {
-        const float4 lo = {x[0], x[1], x[2], x[3]}, hi = {x[4], x[5], x[6], x[7]};
-        *reinterpret_cast<float4*>(p) = lo;
-        *reinterpret_cast<float4*>(p + 16) = hi;
+        typedef float f32x4 __attribute__((ext_vector_type(4)));
+        store_as<NT>(p, f32x4{x[0], x[1], x[2], x[3]});
+        store_as<NT>(p + 16, f32x4{x[4], x[5], x[6], x[7]});
     }
 };
-template <> struct Eight<bf16_t> {
+template <bool NT> struct Eight<bf16_t, NT> {
     u32x4 a;
-    __device__ __forceinline__ void load(const char* p) { a = *reinterpret_cast<const u32x4*>(p); }
+    __device__ __forceinline__ void load(const char* p) { a = load_as<NT, u32x4>(p); }
     __device__ __forceinline__ uint32_t bits(int i) const { return i & 1 ? a[i >> 1] & 0xffff0000u : a[i >> 1] << 16; }
     static __device__ __forceinline__ void store(char* p, const float (&x)[8]) {
         const u32x4 w = {pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
-        *reinterpret_cast<u32x4*>(p) = w;
+        store_as<NT>(p, w);
     }
 };
 
@@ -92,12 +107,12 @@ __device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
 }
 
 // A lane holds 8 elements of a row at a time, so D / 8 lanes a row and 64 / (D / 8) rows a step.
-template <typename T, int FMT, int D, int STEPS>
+template <typename T, int FMT, int D, bool NT, int STEPS>
 __device__ __forceinline__ void write_rows(const Piece& p, const char* rows, int64_t stride_b, char* codes, float* scale, int lane) {
     constexpr int LANES = D / 8, PER = 64 / LANES;
     const int sub = lane / LANES, col = lane % LANES;
     const float old = p.in_block > 0 ? *scale : 0.f;
-    Eight<T> x[STEPS];
+    Eight<T, NT> x[STEPS];
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {
         const int r = i * PER + sub;        // (rows past the last are that one again: they change no maximum)
@@ -139,7 +154,7 @@ __device__ __forceinline__ void write_rows(const Piece& p, const char* rows, int
     if (lane == 0) *scale = s;
 }
 
-template <typename T, int FMT, int D>
+template <typename T, int FMT, int D, bool NT>
 __global__ __launch_bounds__(256) void cache_write_kernel(const RowsArgs a) {
     const int lane = threadIdx.x & 63;
     const long w = static_cast<long>(workgroup_id()) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -151,10 +166,15 @@ __global__ __launch_bounds__(256) void cache_write_kernel(const RowsArgs a) {
     const char* const rows = (kv ? a.v : a.k) + p.row * stride + hk * (kv ? a.v_head : a.k_head) * static_cast<int64_t>(sizeof(T));
     const size_t at = static_cast<size_t>(p.block) * a.Hkv + hk;
     char* const codes = (kv ? a.codes_v : a.codes_k) + at * (BLOCK * D);
-    write_rows<T, FMT, D, D / 8>(p, rows, stride, codes, (kv ? a.scale_v : a.scale_k) + at, lane);
+    float* const scale = (kv ? a.scale_v : a.scale_k) + at;
+    // few rows (a generated token, the ends of a prompt) in as many steps as they take
+    constexpr int PER = 512 / D;
+    if (p.n <= PER) write_rows<T, FMT, D, NT, 1>(p, rows, stride, codes, scale, lane);
+    else if (p.n <= D / 32 * PER) write_rows<T, FMT, D, NT, D / 32>(p, rows, stride, codes, scale, lane);
+    else write_rows<T, FMT, D, NT, D / 8>(p, rows, stride, codes, scale, lane);
 }
 
-template <typename T, int FMT, int D>
+template <typename T, int FMT, int D, bool NT>
 __global__ __launch_bounds__(256) void cache_read_kernel(const RowsArgs a) {
     const int lane = threadIdx.x & 63;
     const long w = static_cast<long>(workgroup_id()) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -169,28 +189,38 @@ __global__ __launch_bounds__(256) void cache_read_kernel(const RowsArgs a) {
     const size_t at = static_cast<size_t>(p.block < 0 ? 0 : p.block) * a.Hkv + hk;
     const char* const codes = (kv ? a.codes_v : a.codes_k) + at * (BLOCK * D) + p.in_block * D;
     const float s = (kv ? a.scale_v : a.scale_k)[at];
+    u32x2 c[STEPS];
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {           // (rows past the last are that one again, so that no load waits for a branch)
+        const int r = i * PER + sub;
+        c[i] = load_as<NT, u32x2>(codes + (r < p.n ? r : p.n - 1) * D + col * 8);
+    }
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {
         const int r = i * PER + sub;
         if (r >= p.n) continue;
-        const u32x2 c = *reinterpret_cast<const u32x2*>(codes + r * D + col * 8);
         float lo[4], hi[4], y[8];
-        Code<FMT>::decode4(c[0], lo);
-        Code<FMT>::decode4(c[1], hi);
+        Code<FMT>::decode4(c[i][0], lo);
+        Code<FMT>::decode4(c[i][1], hi);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             y[e] = p.block < 0 ? 0.f : lo[e] * s;
             y[e + 4] = p.block < 0 ? 0.f : hi[e] * s;
         }
-        Eight<T>::store(rows + r * stride + col * 8 * sizeof(T), y);
+        Eight<T, NT>::store(rows + r * stride + col * 8 * sizeof(T), y);
     }
 }
 
-template <typename T, int FMT, int D>
+template <typename T, int FMT, int D, bool NT>
 void launch(const RowsArgs& a, bool write, hipStream_t st) {
     const dim3 grid = grid_of((a.n_waves + 3) / 4);
-    if (write) cache_write_kernel<T, FMT, D><<<grid, 256, 0, st>>>(a);
-    else cache_read_kernel<T, FMT, D><<<grid, 256, 0, st>>>(a);
+    if (write) cache_write_kernel<T, FMT, D, NT><<<grid, 256, 0, st>>>(a);
+    else cache_read_kernel<T, FMT, D, NT><<<grid, 256, 0, st>>>(a);
+}
+template <typename T, int FMT, int D>
+void launch(const RowsArgs& a, bool write, hipStream_t st) {
+    if (2L * a.T * a.Hkv * D * static_cast<long>(sizeof(T)) > NT_BYTES) launch<T, FMT, D, true>(a, write, st);
+    else launch<T, FMT, D, false>(a, write, st);
 }
 template <typename T, int FMT>
 void launch(const RowsArgs& a, int D, bool write, hipStream_t st) {
