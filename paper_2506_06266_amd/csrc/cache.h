@@ -61,17 +61,28 @@ __device__ __forceinline__ int offset_at(const int32_t* cu, int i, int T) {
 // The request that place `at` of an axis belongs to on which request b begins at cu[b] / unit + pad b: the last one that
 // begins there or before.  (Requests of n rows reach into n / unit + 2 units at most, wherever the first begins, and
 // n / unit + 1 where it begins a unit, so with pad = 2 or 1 each has places enough, without a running sum of units.)
-// All lanes of a wavefront call it; 64 requests are looked at in one trip to memory.
-__device__ __forceinline__ int request_of(const int32_t* cu, int B, int T, int unit_log2, int pad, int at, int lane) {
-    int lo = 0, hi = B;
-    while (hi - lo > 1) {
-        const int step = (hi - lo + 63) >> 6, i = lo + lane * step;
-        const bool there = i < hi && (offset_at(cu, i < hi ? i : lo, T) >> unit_log2) + static_cast<long>(pad) * i <= at;
-        const int n = __builtin_popcountll(__ballot(there));
-        lo += (n > 0 ? n - 1 : 0) * step;
+// All lanes of a wavefront call it; 64 requests are looked at in one trip to memory, and what the caller asks next of the one
+// that is found -- its offsets, its entry of `first` (null: 0) -- comes with the last of them.
+struct Request { int b, from, to, first; };
+__device__ __forceinline__ Request request_of(const int32_t* cu, const int32_t* first, int B, int T, int unit_log2, int pad, int at, int lane) {
+    int lo = 0, hi = B, step, k, c, f;
+    do {
+        step = (hi - lo + 63) >> 6;
+        const int i = lo + lane * step, j = i < B ? i : B;
+        c = offset_at(cu, j, T);
+        f = first ? first[j < B ? j : B - 1] : 0;
+        const int n = __builtin_popcountll(__ballot(i < hi && (c >> unit_log2) + static_cast<long>(pad) * i <= at));
+        k = n > 0 ? n - 1 : 0;
+        lo += k * step;
         hi = hi < lo + step ? hi : lo + step;
-    }
-    return lo;
+    } while (hi - lo > 1);
+    Request r;
+    r.b = lo;
+    r.from = __shfl(c, k);
+    r.to = __shfl(c, k < 63 ? k + 1 : 63);
+    r.first = __shfl(f, k);
+    if (step > 1 || k == 63) r.to = offset_at(cu, lo + 1, T);
+    return r;
 }
 
 }  // namespace cache

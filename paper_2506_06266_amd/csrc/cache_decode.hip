@@ -487,7 +487,7 @@ __global__ __launch_bounds__(256, QO == 16 ? 2 : 1) void cache_decode_split_kern
         });
     };
     for (int p = static_cast<int>(from); p < to; p += 64) {
-        const int n = min(64, to - p), b0 = request_of(a.cu, a.B, INT_MAX, 5, 1, p, lane);
+        const int n = min(64, to - p), b0 = request_of(a.cu, nullptr, a.B, INT_MAX, 5, 1, p, lane).b;
         // the requests of these places: lane k looks at b0 + k, and a lane's place belongs to the last one that begins there or before
         const int bk = min(b0 + lane, a.B - 1), c0 = offset_at(a.cu, bk, INT_MAX), c1 = offset_at(a.cu, bk + 1, INT_MAX);
         const long start = static_cast<long>(c0 >> 5) + bk - p;

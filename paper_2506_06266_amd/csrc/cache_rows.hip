@@ -44,20 +44,22 @@ struct Piece {
 
 __device__ __forceinline__ Piece piece_of(const RowsArgs& a, int place, int lane) {
     Piece p = {0, 0, 0, -1};
-    int b, j, row0, n;
+    int b, j, row0, n, first;
     if (a.cu) {
-        b = request_of(a.cu, a.B, a.T, 6, 2, place, lane);
-        row0 = offset_at(a.cu, b, a.T);
-        n = offset_at(a.cu, b + 1, a.T) - row0;
+        const Request r = request_of(a.cu, a.first, a.B, a.T, 6, 2, place, lane);
+        b = r.b;
+        row0 = r.from;
+        n = r.to - r.from;
+        first = r.first;
         j = place - (row0 >> 6) - 2 * b;
     } else {
         b = place / a.places;
         j = place - b * a.places;
         row0 = b * a.each;
         n = a.each;
+        first = a.first ? a.first[b] : 0;
     }
     if (n <= 0 || j < 0) return p;
-    const int first = a.first ? a.first[b] : 0;
     // (a negative `first` has no blocks; its rows are counted from 0 so that a reader clears them)
     const long f = first < 0 ? 0 : first, blk = f / BLOCK + j;
     const long lo = blk * BLOCK > f ? blk * BLOCK : f, hi = blk * BLOCK + BLOCK < f + n ? blk * BLOCK + BLOCK : f + n;
