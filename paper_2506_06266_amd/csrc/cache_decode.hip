@@ -16,6 +16,8 @@
 #include <limits.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "cache.h"
 
 namespace cart {
@@ -30,6 +32,11 @@ constexpr int STEP = 32;                // keys per step
 // The softmax's reference is the largest score of a query's first step; it is moved where the weights of a later step add up to
 // more than this in a lane (fp32 and bf16 have room for far more; no maximum is formed otherwise).
 constexpr float LIMIT = 65536.f;
+// Own tokens' bytes, half the lengths' bound, from which the codes are read non-temporal: a model's layers have a cache each, and
+// what eight of them read is no longer in the memory-side cache (256 MB) when the next token comes.  us with and without, the cache not
+// read shortly before / read by the call before: 17 MB 9.5 10.4 / 8.4 7.7, 69 MB 17.9 19.8 / 16.0 16.8, 138 MB 29.5 33.2 / 27.5 26.6,
+// 1074 MB 164 185; beside 8192 common slots, which stay in the L2 for it, 128 requests of up to 1024 tokens 48.6 52.1.
+constexpr double NT_BYTES = 32e6;
 constexpr int FEW_ROWS = 2048;          // output rows up to which the join takes four wavefronts a row
 
 struct Sums;
@@ -84,23 +91,25 @@ template <int D, int Q> struct Codes {
     u32x4 k[STEP / PER];                // key PER x + l/CHUNKS, piece l%CHUNKS: whole rows, as they lie in memory
     uint32_t v[OWN][BYTES > 4 ? 2 : 1]; // key of(x, g), bytes BYTES (l%Q)
     static __device__ __forceinline__ int of(int x, int g) { return (x >> 2) * (Q == 16 ? 16 : 8) + 4 * g + (x & 3); }
+    // AUX: 2 for non-temporal
+    template <int AUX>
     __device__ __forceinline__ void load(const char* kp, const char* vp, int n_rows, int lane) {
         const int g = lane / Q, c = lane % Q;
         const __amdgpu_buffer_rsrc_t kb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(kp), 0, n_rows * D, 0x20000);
         const __amdgpu_buffer_rsrc_t vb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(vp), 0, n_rows * D, 0x20000);
 #pragma unroll
-        for (int x = 0; x < STEP / PER; ++x) k[x] = __builtin_amdgcn_raw_buffer_load_b128(kb, x * PER * D + 16 * lane, 0, 0);
+        for (int x = 0; x < STEP / PER; ++x) k[x] = __builtin_amdgcn_raw_buffer_load_b128(kb, x * PER * D + 16 * lane, 0, AUX);
 #pragma unroll
         for (int x = 0; x < OWN; ++x) {
             const int at = of(x, g) * D + BYTES * c;
             if constexpr (BYTES == 8) {
-                const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(vb, at, 0, 0);
+                const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(vb, at, 0, AUX);
                 v[x][0] = w[0];
                 v[x][1] = w[1];
             } else if constexpr (BYTES == 4) {
-                v[x][0] = __builtin_amdgcn_raw_buffer_load_b32(vb, at, 0, 0);
+                v[x][0] = __builtin_amdgcn_raw_buffer_load_b32(vb, at, 0, AUX);
             } else {
-                v[x][0] = __builtin_amdgcn_raw_buffer_load_b16(vb, at, 0, 0);
+                v[x][0] = __builtin_amdgcn_raw_buffer_load_b16(vb, at, 0, AUX);
             }
         }
     }
@@ -298,13 +307,13 @@ __device__ __forceinline__ uint32_t lane_of(uint32_t x, int i) { return static_c
 __device__ __forceinline__ int own_len(const DecodeArgs& a, int c0, int c1) { return min(max(c1 - c0, 0), a.max_own); }
 
 // Takes steps 0 .. n-1 of the list, DEPTH of them in flight.  begin(request) is called ahead of each step.
-template <int FMT, int D, int Q, int DEPTH, typename F>
+template <bool NT, int DEPTH, int FMT, int D, int Q, typename F>
 __device__ __forceinline__ void run(const DecodeArgs& a, const Steps& st, int n, int hk, Rows<FMT, D, Q>& rows, Keys<D>& keys, int lane, F&& begin) {
     Codes<D, Q> x[DEPTH];
     auto load = [&](Codes<D, Q>& y, int i) __attribute__((always_inline)) {
         const int at = min(i, n - 1), rows = i < n ? max(lane_of(st.rows, at), 0) : 0;
         const size_t from = static_cast<size_t>(lane_of(st.at_hi, at)) << 32 | lane_of(st.at_lo, at);
-        y.load(a.k + from, a.v + from, rows, lane);
+        y.template load<NT ? 2 : 0>(a.k + from, a.v + from, rows, lane);
     };
 #pragma unroll
     for (int j = 0; j < DEPTH; ++j) load(x[j], j);
@@ -375,7 +384,7 @@ __device__ __forceinline__ void leave(const DecodeArgs& a, long slot, size_t row
 
 // ---- every (request, KV head) by itself: a workgroup takes one of n_cuts pieces, of `cut` steps, of its sequence -- the segments'
 // steps, then its own -- its four wavefronts a quarter each, joined in LDS.  With one piece it writes the output.
-template <int FMT, int D, int Q>
+template <int FMT, int D, int Q, bool NT>
 __global__ __launch_bounds__(256, Q == 16 ? 3 : 1) void cache_decode_each_kernel(const DecodeArgs a) {
     __shared__ union Lds {
         Join<D, Q, 4> join;
@@ -402,7 +411,7 @@ __global__ __launch_bounds__(256, Q == 16 ? 3 : 1) void cache_decode_each_kernel
             if (s + lane < n_shared) st.of_segments(a, hk, D, s + lane);
             else st.of_request(a, hk, D, static_cast<int>(b), s + lane - n_shared, n_own);
         }
-        run<FMT, D, Q, 2>(a, st, min(64, w1 - s), hk, rows, lds.keys[wv], lane, [](int) {});
+        run<NT, 2>(a, st, min(64, w1 - s), hk, rows, lds.keys[wv], lane, [](int) {});
     }
     __syncthreads();                                    // (the keys' place)
     lds.join.put(wv, rows, lane);
@@ -429,7 +438,7 @@ __device__ __forceinline__ int range_len(const DecodeArgs& a) {
     const int places = (offset_at(a.cu, a.B, INT_MAX) >> 5) + a.B;
     return (places + a.n_ranges - 1) / a.n_ranges;
 }
-template <int FMT, int D, int QS, int QO>
+template <int FMT, int D, int QS, int QO, bool NT>
 __global__ __launch_bounds__(256, QO == 16 ? 2 : 1) void cache_decode_split_kernel(const DecodeArgs a) {
     __shared__ union Lds {
         Join<D, QS, 4> join;
@@ -451,7 +460,7 @@ __global__ __launch_bounds__(256, QO == 16 ? 2 : 1) void cache_decode_split_kern
         for (int s = p0 + n * wv / 4; s < w1; s += 64) {
             Steps st;
             if (s + lane < w1) st.of_segments(a, hk, D, s + lane);
-            run<FMT, D, QS, 2>(a, st, min(64, w1 - s), hk, rows, lds.keys[wv], lane, [](int) {});
+            run<false, 2>(a, st, min(64, w1 - s), hk, rows, lds.keys[wv], lane, [](int) {});
         }
         __syncthreads();                                // (the keys' place)
         lds.join.put(wv, rows, lane);
@@ -501,7 +510,7 @@ __global__ __launch_bounds__(256, QO == 16 ? 2 : 1) void cache_decode_split_kern
         const int r0 = __shfl(c0, k), r1 = __shfl(c1, k), b = b0 + k;
         Steps st;
         if (lane < n) st.of_request(a, hk, D, b, p + lane - (r0 >> 5) - b, own_len(a, r0, r1));
-        run<FMT, D, QO, 2>(a, st, n, hk, rows, lds.keys[wv], lane, [&](int at) __attribute__((always_inline)) {
+        run<NT, 2>(a, st, n, hk, rows, lds.keys[wv], lane, [&](int at) __attribute__((always_inline)) {
             const int request = lane_of(st.request, at);
             if (request == current) return;
             if (current >= 0) {
@@ -612,6 +621,10 @@ constexpr int MIN_CUT = 4;              // fewest steps of a piece: one a wavefr
 // most workgroups of pieces, and wavefronts of ranges, per CU
 constexpr int MAX_PIECES = 16, MAX_RANGES = 8;
 
+double own_bytes(const cart_cache_decode_desc& d, const cart_cache& c) {
+    return 0.5 * static_cast<double>(d.B) * c.Hkv * steps_of(d.max_own_len) * STEP * 2 * c.D;
+}
+
 // The faster by an estimate (us; `own` half full on average), whose figures are those of sweeps of all forms, 18 problems without
 // segments and 23 with (256 CUs, head_dim 128, e4m3):
 //   every (request, KV head) by itself, in n pieces: 5.3 and 0.14 a step of the longest piece (its four wavefronts share it) where the chip
@@ -628,7 +641,7 @@ Plan plan_of(const cart_cache_decode_desc& d, const cart_cache& c, const cart_ca
     for (int s = 0; s < d.n_shared; ++s) steps += steps_of(shared[s].p);
     const long own = steps_of(d.max_own_len), all = steps + own, group = d.Hq / c.Hkv;
     const long rows = d.B * group, pairs = static_cast<long>(d.B) * c.Hkv, out = static_cast<long>(d.B) * d.Hq;
-    const double chip = static_cast<double>(cus) / 256, own_mb = 0.5 * static_cast<double>(pairs * own) * STEP * 2 * c.D * 1e-6 / chip;
+    const double chip = static_cast<double>(cus) / 256, own_mb = own_bytes(d, c) * 1e-6 / chip;
 
     double each_us = 0;
     for (long n = 1; n == 1 || (n * MIN_CUT <= all && n * pairs <= MAX_PIECES * cus); n *= 2) {
@@ -674,16 +687,16 @@ long most_slots(const cart_cache_decode_desc& d, const cart_cache& c, const cart
     return pieces > parts + ranges ? pieces : parts + ranges;
 }
 
-template <int FMT, int D>
+template <int FMT, int D, bool NT>
 void launch(const DecodeArgs& a, const Plan& p, hipStream_t st) {
     const dim3 grid = grid_of(p.n_wg);
     if (p.n_cuts > 0) {
-        if (a.G <= 16) cache_decode_each_kernel<FMT, D, 16><<<grid, 256, 0, st>>>(a);
-        else cache_decode_each_kernel<FMT, D, 32><<<grid, 256, 0, st>>>(a);
+        if (a.G <= 16) cache_decode_each_kernel<FMT, D, 16, NT><<<grid, 256, 0, st>>>(a);
+        else cache_decode_each_kernel<FMT, D, 32, NT><<<grid, 256, 0, st>>>(a);
         if (p.n_cuts == 1) return;
-    } else if (a.G > 16) cache_decode_split_kernel<FMT, D, 32, 32><<<grid, 256, 0, st>>>(a);
-    else if (static_cast<long>(a.B) * a.G > 16) cache_decode_split_kernel<FMT, D, 32, 16><<<grid, 256, 0, st>>>(a);
-    else cache_decode_split_kernel<FMT, D, 16, 16><<<grid, 256, 0, st>>>(a);
+    } else if (a.G > 16) cache_decode_split_kernel<FMT, D, 32, 32, NT><<<grid, 256, 0, st>>>(a);
+    else if (static_cast<long>(a.B) * a.G > 16) cache_decode_split_kernel<FMT, D, 32, 16, NT><<<grid, 256, 0, st>>>(a);
+    else cache_decode_split_kernel<FMT, D, 16, 16, NT><<<grid, 256, 0, st>>>(a);
     const long rows = static_cast<long>(a.B) * a.Hq;
     if (rows <= FEW_ROWS) cache_decode_join_kernel<D, 4><<<grid_of(rows), 256, 0, st>>>(a);
     else cache_decode_join_kernel<D, 1><<<grid_of((rows + 3) / 4), 256, 0, st>>>(a);
@@ -719,13 +732,18 @@ int launch_cache_decode(const cart_cache_decode_desc& d, const cart_cache& c, fl
     a.n_shared_wg = p.n_shared_wg;
     a.part_o = static_cast<float*>(ws);             // (first: its rows are multiples of 16 bytes)
     a.part_sums = reinterpret_cast<Sums*>(a.part_o + static_cast<size_t>(p.slots) * d.Hq * c.D);
-    if (c.D == 64) {
-        if (c.format == CART_I8) launch<CART_I8, 64>(a, p, st);
-        else launch<CART_E4M3, 64>(a, p, st);
-    } else {
-        if (c.format == CART_I8) launch<CART_I8, 128>(a, p, st);
-        else launch<CART_E4M3, 128>(a, p, st);
-    }
+    auto go = [&](auto nt) {
+        constexpr bool NT = decltype(nt)::value;
+        if (c.D == 64) {
+            if (c.format == CART_I8) launch<CART_I8, 64, NT>(a, p, st);
+            else launch<CART_E4M3, 64, NT>(a, p, st);
+        } else {
+            if (c.format == CART_I8) launch<CART_I8, 128, NT>(a, p, st);
+            else launch<CART_E4M3, 128, NT>(a, p, st);
+        }
+    };
+    if (own_bytes(d, c) >= NT_BYTES) go(std::true_type{});
+    else go(std::false_type{});
     return static_cast<int>(hipGetLastError());
 }
 

@@ -377,6 +377,20 @@ def test_rows_past_the_bound_are_not_attended_and_outputs_stay_in_place(fmt):
     check_decode(o[1:4], lse[1:4], c.decode_ref(q.cpu(), shared, table, [min(n, bound) for n in lens]), 128)
 
 
+@pytest.mark.parametrize("fmt", FMT)
+@pytest.mark.parametrize("Hq,Hkv,D", [(8, 2, 64), (32, 1, 64), (32, 8, 128), (24, 1, 128)])
+@pytest.mark.parametrize("lens", [[100, 0, 33, 700, 64], [300]], ids=["five", "one"])
+@pytest.mark.parametrize("seg_p", [[], [2500]], ids=["alone", "behind"])
+def test_a_bound_far_above_the_lengths(seg_p, lens, Hq, Hkv, D, fmt):
+    """33 MB of codes by the bound, a table as wide, a few tokens."""
+    c, table, shared = filled(lens, seg_p, Hkv, D, fmt, seed=Hq + D)
+    wide = np.full((len(lens), -(-33000000 // (len(lens) * Hkv * D * 64))), -1)
+    wide[:, :table.shape[1]] = table
+    q = rand(len(lens), Hq, D, seed=79, spread=0.5).bfloat16()
+    o, lse = cb.cart_cache_decode(q.cuda(), c.gpu, [(i32(b), p) for b, p in shared], i32(wide), i32(offsets(lens)), 64 * wide.shape[1])
+    check_decode(o, lse, c.decode_ref(q, shared, table, lens), D)
+
+
 def test_blocks_past_four_gigabytes():
     """Codes whose offset passes 2^32 bytes; the scales' offsets do not."""
     Hkv, D, n_blocks = 8, 128, 70000
