@@ -438,8 +438,9 @@ __device__ __forceinline__ int range_len(const DecodeArgs& a) {
     const int places = (offset_at(a.cu, a.B, INT_MAX) >> 5) + a.B;
     return (places + a.n_ranges - 1) / a.n_ranges;
 }
-template <int FMT, int D, int QS, int QO, bool NT>
-__global__ __launch_bounds__(256, QO == 16 ? 2 : 1) void cache_decode_split_kernel(const DecodeArgs a) {
+template <int FMT, int D, int QS, bool NT>
+__global__ __launch_bounds__(256, 2) void cache_decode_split_kernel(const DecodeArgs a) {
+    constexpr int QO = 16;                              // (at most 16 queries a KV head: see plan_of)
     __shared__ union Lds {
         Join<D, QS, 4> join;
         Keys<D> keys[4];
@@ -626,14 +627,16 @@ double own_bytes(const cart_cache_decode_desc& d, const cart_cache& c) {
 }
 
 // The faster by an estimate (us; `own` half full on average), whose figures are those of sweeps of all forms, 18 problems without
-// segments and 23 with (256 CUs, head_dim 128, e4m3):
+// segments and 44 with (256 CUs, head_dim 128 unless said):
 //   every (request, KV head) by itself, in n pieces: 5.3 and 0.14 a step of the longest piece (its four wavefronts share it) where the chip
-//     is not full, 0.6 a step and SIMD where it is -- the segments' steps again for every request --, or the own bytes at 5.2 TB/s;
-//     the second launch 4.5 and its partial results.  32 requests of up to 1024 tokens: n = 1 10.9, 2 15.3, 4 17.8; one of 16384: n = 1
-//     76, 4 26.8, 16 14.1, 32 13.6; 128 of 2049 .. 3071 behind 2048 common slots 128, split 134;
-//   split: 11, the second launch's rows, and the longer of a segment wavefront's 0.95 a step and the own bytes at 5 TB/s; as many parts as
-//     give each CU one workgroup: 128 requests of up to 1024 tokens, 8192 slots: 1 part 70, 2 53.3, 3 56.8, 4 68.9 (by itself 146);
-//     64 requests: 2 parts 38.5, 4 29.2, 8 40.5; 23 (69 rows), 5003 slots: 4 19.5, 8 17.1 (by itself 25.9).
+//     is not full, 0.6 a segment's step and SIMD -- every request's again -- and the own bytes at 6.2 TB/s; the second launch 3 and its
+//     partial results.  32 requests of up to 1024 tokens: n = 1 10.9, 2 15.3, 4 17.8; one of 16384: n = 1 76, 4 26.8, 16 14.1, 32 13.6;
+//   split: 13, the second launch's rows, and the longer of a segment wavefront's 0.73 a step and the own bytes, with some of the other; as
+//     many parts as give each CU one workgroup (128 requests of up to 1024 tokens, 8192 slots: 1 part 70, 2 53.3, 3 56.8, 4 68.9).
+//   By itself / split: 128 requests of up to 1024 tokens behind 8192 slots 146 / 48.6, of 512 behind 1024 36.4 / 26.5, of 1024 behind 512
+//   37.0 / 37.2; 64 of 512 behind 512 16.0 / 22.2; 16 of 16384 behind 8192 83 / 60.6; 1 of 131072 behind 2048 31.8 / 41.1; head_dim 64: 128
+//   of 2048 behind 2048 54.0 / 34.3, 32 of 1024 behind 1024 11.3 / 14.8.  The worst choices cost 8 % (4 of 16384 behind 8192: 26.3 / 28.4).
+//   With more than 16 queries a KV head shares its keys among enough of them by itself: 25.2 / 30.1, 41.0 / 59.0, 36.0 / 33.9 of 9.
 Plan plan_of(const cart_cache_decode_desc& d, const cart_cache& c, const cart_cache_segment* shared) {
     Plan p = {}, q = {};
     const long cus = device_cus();
@@ -641,14 +644,14 @@ Plan plan_of(const cart_cache_decode_desc& d, const cart_cache& c, const cart_ca
     for (int s = 0; s < d.n_shared; ++s) steps += steps_of(shared[s].p);
     const long own = steps_of(d.max_own_len), all = steps + own, group = d.Hq / c.Hkv;
     const long rows = d.B * group, pairs = static_cast<long>(d.B) * c.Hkv, out = static_cast<long>(d.B) * d.Hq;
-    const double chip = static_cast<double>(cus) / 256, own_mb = own_bytes(d, c) * 1e-6 / chip;
+    const double chip = static_cast<double>(cus) / 256, own_us = own_bytes(d, c) / 6.2e6 / chip;
 
     double each_us = 0;
     for (long n = 1; n == 1 || (n * MIN_CUT <= all && n * pairs <= MAX_PIECES * cus); n *= 2) {
         const double full = static_cast<double>(pairs * n) / static_cast<double>(6 * cus);
-        const double us = 5.3 + fmax(fmax(0.14 * static_cast<double>((all + n - 1) / n) * fmax(1.0, full),
-                                          0.6 * static_cast<double>(pairs) * (static_cast<double>(steps) + 0.5 * static_cast<double>(own)) / static_cast<double>(4 * cus)),
-                                     own_mb / 5.2) + (n > 1 ? 4.5 + static_cast<double>(out * n) / 900 : 0.0);
+        const double us = 5.3 + fmax(0.14 * static_cast<double>((all + n - 1) / n) * fmax(1.0, full),
+                                     0.6 * static_cast<double>(pairs * steps) / static_cast<double>(4 * cus) + own_us) +
+                          (n > 1 ? 3 + static_cast<double>(out * n) / 1000 : 0.0);
         if (n > 1 && us >= each_us) continue;
         each_us = us;
         p.cut = static_cast<int>(all > 0 ? (all + n - 1) / n : 1);
@@ -656,13 +659,14 @@ Plan plan_of(const cart_cache_decode_desc& d, const cart_cache& c, const cart_ca
     p.n_cuts = static_cast<int>(all > 0 ? (all + p.cut - 1) / p.cut : 1);
     p.n_wg = pairs * p.n_cuts;
     p.slots = p.n_cuts == 1 ? 0 : static_cast<long>(p.n_cuts) * d.B;
-    if (steps == 0) return p;
+    if (steps == 0 || group > 16) return p;
 
     const int per = rows > 16 ? 32 : 16;
     q.n_rb = static_cast<int>((rows + per - 1) / per);
     const long one = static_cast<long>(q.n_rb) * c.Hkv, want = (cus + one - 1) / one, most = (steps + 3) / 4;
     q.n_parts = static_cast<int>(want < most ? want : most);
-    const double split_us = 11 + static_cast<double>(out) / 700 + fmax(0.95 * static_cast<double>(steps) / (4.0 * q.n_parts), own_mb / 5.0);
+    const double shared_us = 0.73 * static_cast<double>(steps) / (4.0 * q.n_parts);
+    const double split_us = 13 + static_cast<double>(out) / 1200 + fmax(shared_us, own_us) + 0.3 * fmin(shared_us, own_us);
     if (each_us <= split_us) return p;
     q.n_shared_wg = one * q.n_parts;
     q.slots = static_cast<long>(q.n_parts) * d.B;
@@ -694,9 +698,8 @@ void launch(const DecodeArgs& a, const Plan& p, hipStream_t st) {
         if (a.G <= 16) cache_decode_each_kernel<FMT, D, 16, NT><<<grid, 256, 0, st>>>(a);
         else cache_decode_each_kernel<FMT, D, 32, NT><<<grid, 256, 0, st>>>(a);
         if (p.n_cuts == 1) return;
-    } else if (a.G > 16) cache_decode_split_kernel<FMT, D, 32, 32, NT><<<grid, 256, 0, st>>>(a);
-    else if (static_cast<long>(a.B) * a.G > 16) cache_decode_split_kernel<FMT, D, 32, 16, NT><<<grid, 256, 0, st>>>(a);
-    else cache_decode_split_kernel<FMT, D, 16, 16, NT><<<grid, 256, 0, st>>>(a);
+    } else if (static_cast<long>(a.B) * a.G > 16) cache_decode_split_kernel<FMT, D, 32, NT><<<grid, 256, 0, st>>>(a);
+    else cache_decode_split_kernel<FMT, D, 16, NT><<<grid, 256, 0, st>>>(a);
     const long rows = static_cast<long>(a.B) * a.Hq;
     if (rows <= FEW_ROWS) cache_decode_join_kernel<D, 4><<<grid_of(rows), 256, 0, st>>>(a);
     else cache_decode_join_kernel<D, 1><<<grid_of((rows + 3) / 4), 256, 0, st>>>(a);

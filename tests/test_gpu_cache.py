@@ -391,6 +391,22 @@ def test_a_bound_far_above_the_lengths(seg_p, lens, Hq, Hkv, D, fmt):
     check_decode(o, lse, c.decode_ref(q, shared, table, lens), D)
 
 
+@pytest.mark.parametrize("fmt", FMT)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("B,P", [(4, 20000), (4, 19999), (16, 8000), (19, 7990)])
+def test_long_segments_by_their_own(B, P, D, fmt):
+    """Segments far longer than the requests, that list their blocks several times; the bound at the lengths and far above them."""
+    Hq, Hkv, lens = 32, 8, [(67 * i) % 300 for i in range(B)]
+    c, table, shared = filled(lens, [1280, 100], Hkv, D, fmt, seed=B + D)
+    many = [(np.tile(shared[0][0], -(-P // 1280)), P), shared[1]]
+    q = rand(B, Hq, D, seed=80, spread=0.5).bfloat16()
+    ref = c.decode_ref(q, many, table, lens)
+    check_decode(*run_decode(c, q, many, table, lens), ref, D)
+    wide = np.full((B, -(-33000000 // (B * Hkv * D * 64))), -1)
+    wide[:, :table.shape[1]] = table
+    check_decode(*cb.cart_cache_decode(q.cuda(), c.gpu, [(i32(b), p) for b, p in many], i32(wide), i32(offsets(lens)), 64 * wide.shape[1]), ref, D)
+
+
 def test_blocks_past_four_gigabytes():
     """Codes whose offset passes 2^32 bytes; the scales' offsets do not."""
     Hkv, D, n_blocks = 8, 128, 70000
