@@ -147,17 +147,19 @@ typedef struct {
     int32_t D;              /* head_dim: 64 or 128 (else CART_ERR_UNSUPPORTED) */
     cart_cache_format format;
     void *k, *v;            /* [n_blocks,Hkv,64,D] codes, 16-byte aligned */
-    float *k_scale, *v_scale;   /* [n_blocks,Hkv]; every scale > 0 (or NaN, see cart_cache_write), 4-byte aligned */
+    float *k_scale, *v_scale;   /* [n_blocks,Hkv]; every scale a normal number
+                               > 0 (or NaN, see cart_cache_write), 4-byte aligned */
 } cart_cache;
 
 /* Rows of K and V on their way into or out of a cart_cache. */
 typedef struct {
     int32_t T;              /* rows of this call, all requests, >= 0 */
-    int32_t B;              /* requests, >= 1 */
+    int32_t B;              /* requests, >= 1; (T / 64 + 2 B) Hkv up to 2^31 */
     int32_t max_blocks;     /* row length of the block table, >= 1 */
     cart_dtype dtype;       /* of the rows: CART_F32 or CART_BF16 */
     /* element (t, h, d) of k lies at k + t k_row_stride + h k_head_stride + d, likewise of v; strides in
-     * elements, >= 0, whole multiples of 16 bytes ([T,Hkv,D]: Hkv D and D; [Hkv,T,D]: D and T D) */
+     * elements, >= 0, whole multiples of 16 bytes ([T,Hkv,D]: Hkv D and D; [Hkv,T,D]: D and T D).  Rows to read into
+     * must not overlap (a stride of 0 over more than one row or head is CART_ERR_SHAPE there). */
     int64_t k_row_stride, k_head_stride, v_row_stride, v_head_stride;
 } cart_cache_rows;
 
@@ -169,7 +171,7 @@ typedef struct {
 
 /* Decode step over a cart_cache. */
 typedef struct {
-    int32_t B;              /* requests, >= 1 */
+    int32_t B;              /* requests, 1 .. 2^30; B Hq D up to 2^38 */
     int32_t Hq;             /* query heads, a multiple of the cache's Hkv, at most 32 a KV head */
     int32_t n_shared;       /* 0..CART_MAX_SEGMENTS segments every request attends over */
     int32_t max_blocks;     /* row length of the block table, >= 0 (0: no request has rows of its own) */
@@ -326,7 +328,8 @@ cart_status cart_decode_composed(const cart_decode_composed_desc *desc, const vo
  * the block's new rows and qmax = 127 (CART_I8) or 448 (CART_E4M3):
  *   scale = the smallest power of two with m <= qmax scale, 2^-64 at least; and where the block held
  *           rows before (first[b] is not its first token), at least the scale it had;
- *   code  = x / scale, rounded to the nearest representable value, half to even.
+ *   code  = x / scale, rounded to the nearest representable value, half to even (x times 1 / scale in fp32: exact for
+ *           powers of two, the only scales that this call leaves where it begins blocks).
  * A scale that grows has the codes of the rows before first[b] rounded again (they keep value / new
  * scale; each growth at least doubles the scale, so all roundings of a value add up to less than
  * scale (CART_I8), and are exact but for the smallest values (CART_E4M3)).  Rows of the block past
@@ -340,8 +343,8 @@ cart_status cart_decode_composed(const cart_decode_composed_desc *desc, const vo
  *   table    [B,max_blocks] int32 (device)                 in
  *   the cache's codes and scales                           in, out
  * Rows past 64 max_blocks tokens, of a request with a negative `first`, or whose block id is outside
- * [0, n_blocks) are not written.  No two requests of a call may touch the same block (their codes
- * and its scale are unspecified then).  No workspace.
+ * [0, n_blocks) are not written.  No block may be touched from two places of a call, two requests'
+ * or two of one's row of `table` (its codes and its scale are unspecified then).  No workspace.
  */
 cart_status cart_cache_write(const cart_cache *cache, const cart_cache_rows *rows, const void *k,
                              const void *v, const int32_t *cu_rows, const int32_t *first,

@@ -117,6 +117,7 @@ cart_status check_cache_rows(const cart_cache* c, const cart_cache_rows* r, cons
     if (r->T < 0 || r->B < 1 || r->max_blocks < 1) return CART_ERR_SHAPE;
     if (r->dtype != CART_F32 && r->dtype != CART_BF16) return CART_ERR_UNSUPPORTED;
     if (!cu && r->T % r->B != 0) return CART_ERR_SHAPE;
+    if ((r->T / CART_CACHE_BLOCK + 2.0 * r->B) * c->Hkv > 2147483648.0) return CART_ERR_SHAPE;     // (half the wavefronts)
     const int64_t strides[4] = {r->k_row_stride, r->k_head_stride, r->v_row_stride, r->v_head_stride};
     for (int64_t x : strides) {
         if (x < 0 || x > (INT64_C(1) << 40)) return CART_ERR_SHAPE;
@@ -132,13 +133,13 @@ cart_status check_cache_decode(const cart_cache_decode_desc* d, const cart_cache
     if (!d) return CART_ERR_NULL;
     cart_status s = check_cache(c, pointers);
     if (s != CART_OK) return s;
-    if (d->B < 1 || d->Hq < 1 || d->Hq % c->Hkv != 0) return CART_ERR_SHAPE;
+    if (d->B < 1 || d->B > (1 << 30) || d->Hq < 1 || d->Hq % c->Hkv != 0) return CART_ERR_SHAPE;
     if (d->dtype != CART_BF16 || d->Hq / c->Hkv > 32) return CART_ERR_UNSUPPORTED;
     if (d->n_shared < 0 || d->n_shared > CART_MAX_SEGMENTS) return CART_ERR_SHAPE;
     if (d->max_blocks < 0 || d->max_own_len < 0 || d->max_own_len > (1 << 30) ||
         d->max_own_len > static_cast<int64_t>(d->max_blocks) * CART_CACHE_BLOCK)
         return CART_ERR_SHAPE;
-    if (static_cast<double>(d->B) * d->Hq * c->D > 1099511627776.0) return CART_ERR_SHAPE;
+    if (static_cast<double>(d->B) * d->Hq * c->D > 274877906944.0) return CART_ERR_SHAPE;
     if (!(d->softmax_scale >= 0.f) || isinf(d->softmax_scale)) return CART_ERR_SHAPE;
     if (d->n_shared > 0 && !shared) return CART_ERR_NULL;
     for (int i = 0; i < d->n_shared; ++i) {
@@ -391,6 +392,9 @@ cart_status cart_cache_read(const cart_cache* c, const cart_cache_rows* r, void*
                             const int32_t* first, const int32_t* table, void* stream) {
     cart_status s = check_cache_rows(c, r, k, v, cu_rows, first, table);
     if (s != CART_OK || r->T == 0) return s;
+    // (rows that all lie in one place can be written from, not read into)
+    if ((r->T > 1 && (r->k_row_stride == 0 || r->v_row_stride == 0)) || (c->Hkv > 1 && (r->k_head_stride == 0 || r->v_head_stride == 0)))
+        return CART_ERR_SHAPE;
     int e = cart::launch_cache_rows(*c, *r, k, v, cu_rows, first, table, false, static_cast<hipStream_t>(stream));
     return e == 0 ? CART_OK : CART_ERR_LAUNCH;
 }

@@ -13,6 +13,7 @@
 // 16), so 32 queries take it where there are more than 16.
 // Codes become bf16 exactly; the block's K scale goes into the exponent's factor, its V scale into the exponent.  The weights are
 // rounded to bf16, the second product's operand type (2^-9 of each, as in the 16-bit decode); sums, references and O are fp32.
+#include <float.h>
 #include <limits.h>
 #include <math.h>
 
@@ -284,6 +285,7 @@ struct Steps {
         at_lo = static_cast<uint32_t>(from);
         at_hi = static_cast<uint32_t>(from >> 32);
         c = a.c * a.k_scale[at];
+        c = c < FLT_MIN ? FLT_MIN : c;  // (not 0, by which the -inf of a key that does not exist would become NaN)
         lv = fast_log2(a.v_scale[at]);
         unscale = fast_exp2(-lv);
     }

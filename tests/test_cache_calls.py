@@ -43,6 +43,11 @@ def test_rows_are_refused(lib, name):
     assert call(cache(), rows(), k=None) == 1 and call(cache(), rows(), v=None) == 1 and call(cache(), rows(), table=None) == 1
     assert call(cache(), rows(), k=P + 8) == 6 and call(cache(), rows(), table=P + 2) == 6 and call(cache(), rows(), cu=P + 1) == 6
     assert call(cache(), rows(T=7), cu=None) == 2               # 7 rows of 3 requests
+    # more wavefronts than a launch counts
+    assert call(cache(), rows(B=2 ** 30, T=1)) == 2 and call(cache(Hkv=2 ** 20), rows(B=2 ** 10 + 1, T=1)) == 2
+    if name == "cart_cache_read":
+        for kw in (dict(k_row_stride=0), dict(k_head_stride=0), dict(v_row_stride=0), dict(v_head_stride=0)):
+            assert call(cache(), rows(**kw)) == 2, kw
     # no row at all: nothing to launch, nothing to point to
     assert call(cache(), rows(T=0), k=None, v=None) == 0 and call(cache(), rows(T=0), k=None, v=None, cu=None, first=None, table=None) == 0
 
@@ -60,7 +65,8 @@ def test_decode_is_refused(lib):
     for kw, status in [(dict(B=0), 2), (dict(Hq=0), 2), (dict(Hq=7), 2), (dict(Hq=66), 3), (dict(n_shared=-1), 2), (dict(n_shared=9), 2),
                        (dict(max_blocks=-1), 2), (dict(max_own_len=-1), 2), (dict(max_own_len=257), 2), (dict(dtype=cb.CART_F32), 3),
                        (dict(softmax_scale=-1.0), 2), (dict(softmax_scale=float("nan")), 2), (dict(softmax_scale=float("inf")), 2),
-                       (dict(max_blocks=2 ** 31 - 1, max_own_len=2 ** 30 + 1), 2), (dict(n_shared=1), 1)]:
+                       (dict(max_blocks=2 ** 31 - 1, max_own_len=2 ** 30 + 1), 2), (dict(n_shared=1), 1), (dict(B=2 ** 30 + 1), 2),
+                       (dict(B=2 ** 30, Hq=8), 2)]:
         assert call(desc(**kw)) == status, kw
         assert lib.cart_cache_decode_workspace(C.byref(desc(**kw)), C.byref(cache()), None) == 0, kw
     assert call(None) == 1 and call(desc(), q=None) == 1 and call(desc(), o=None) == 1 and call(desc(), table=None) == 1 and call(desc(), cu=None) == 1

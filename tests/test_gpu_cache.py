@@ -354,6 +354,15 @@ def test_decode_of_scores_far_apart(fmt):
 
 
 @pytest.mark.parametrize("fmt", FMT)
+def test_decode_of_scores_below_the_smallest_number(fmt):
+    """A softmax scale and keys whose product fp32 does not hold: equal weights, also beside keys that do not exist."""
+    lens = [40, 1, 64, 0, 130]
+    c, table, shared = filled(lens, [70], 2, 128, fmt, seed=8, k_std=2.0 ** -70)
+    q = rand(5, 8, 128, seed=9, spread=0.5).bfloat16()
+    check_decode(*run_decode(c, q, shared, table, lens, scale=1e-30), c.decode_ref(q, shared, table, lens, 1e-30), 128)
+
+
+@pytest.mark.parametrize("fmt", FMT)
 def test_decode_takes_scales_that_are_no_powers_of_two(fmt):
     c, table, shared = filled([200, 31], [70], 2, 128, fmt, seed=3)
     g = torch.Generator().manual_seed(4)
