@@ -24,6 +24,15 @@
 namespace cart {
 using namespace cache;
 
+// How a call is cut (host only: the planner is tested without a GPU)
+struct CachePlan {
+    int n_rb, n_parts, n_ranges;        // the segments by their own (n_cuts == 0)
+    int n_cuts, cut;                    // every (request, KV head) by itself
+    long n_shared_wg, n_wg;
+    long slots;                         // partial results of Hq rows
+};
+CachePlan cache_decode_plan(const cart_cache_decode_desc& d, const cart_cache& c, const cart_cache_segment* shared);
+
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -442,7 +451,7 @@ __device__ __forceinline__ int range_len(const DecodeArgs& a) {
 }
 template <int FMT, int D, int QS, bool NT>
 __global__ __launch_bounds__(256, 2) void cache_decode_split_kernel(const DecodeArgs a) {
-    constexpr int QO = 16;                              // (at most 16 queries a KV head: see plan_of)
+    constexpr int QO = 16;                              // (at most 16 queries a KV head: see cache_decode_plan)
     __shared__ union Lds {
         Join<D, QS, 4> join;
         Keys<D> keys[4];
@@ -614,12 +623,6 @@ __global__ __launch_bounds__(256) void cache_decode_join_kernel(const DecodeArgs
     if (sub == 0) finish(a, static_cast<size_t>(row), D, d, x, t);
 }
 
-struct Plan {
-    int n_rb, n_parts, n_ranges;        // the segments by their own (n_cuts == 0)
-    int n_cuts, cut;                    // every (request, KV head) by itself
-    long n_shared_wg, n_wg;
-    long slots;                         // partial results of Hq rows
-};
 constexpr int MIN_CUT = 4;              // fewest steps of a piece: one a wavefront
 // most workgroups of pieces, and wavefronts of ranges, per CU
 constexpr int MAX_PIECES = 16, MAX_RANGES = 8;
@@ -627,6 +630,35 @@ constexpr int MAX_PIECES = 16, MAX_RANGES = 8;
 double own_bytes(const cart_cache_decode_desc& d, const cart_cache& c) {
     return 0.5 * static_cast<double>(d.B) * c.Hkv * steps_of(d.max_own_len) * STEP * 2 * c.D;
 }
+
+// Partial results that no plan of these sizes or smaller ones exceeds (slots of Hq rows), so that a workspace for a program's largest
+// call serves its others.  Parts: cus / (n_rb Hkv) + 1 for each request at most, and n_rb >= rows / 32.
+long most_slots(const cart_cache_decode_desc& d, const cart_cache& c, const cart_cache_segment* shared) {
+    const long cus = device_cus(), B = d.B, own = steps_of(d.max_own_len);
+    long steps = 0;
+    for (int s = 0; s < d.n_shared; ++s) steps += steps_of(shared[s].p);
+    auto least = [](long x, long y) { return x < y ? x : y; };
+    const long pieces = least(((steps + own) / MIN_CUT + 1) * B, MAX_PIECES * cus / c.Hkv + B);
+    const long parts = least((steps + 3) / 4 * B, 32 * cus / d.Hq + B + 1);
+    const long ranges = own > 0 ? least(B * (own + 1), MAX_RANGES * cus / c.Hkv + 1) + B : 0;
+    return pieces > parts + ranges ? pieces : parts + ranges;
+}
+
+template <int FMT, int D, bool NT>
+void launch(const DecodeArgs& a, const CachePlan& p, hipStream_t st) {
+    const dim3 grid = grid_of(p.n_wg);
+    if (p.n_cuts > 0) {
+        if (a.G <= 16) cache_decode_each_kernel<FMT, D, 16, NT><<<grid, 256, 0, st>>>(a);
+        else cache_decode_each_kernel<FMT, D, 32, NT><<<grid, 256, 0, st>>>(a);
+        if (p.n_cuts == 1) return;
+    } else if (static_cast<long>(a.B) * a.G > 16) cache_decode_split_kernel<FMT, D, 32, NT><<<grid, 256, 0, st>>>(a);
+    else cache_decode_split_kernel<FMT, D, 16, NT><<<grid, 256, 0, st>>>(a);
+    const long rows = static_cast<long>(a.B) * a.Hq;
+    if (rows <= FEW_ROWS) cache_decode_join_kernel<D, 4><<<grid_of(rows), 256, 0, st>>>(a);
+    else cache_decode_join_kernel<D, 1><<<grid_of((rows + 3) / 4), 256, 0, st>>>(a);
+}
+
+}  // namespace
 
 // The faster by an estimate (us; `own` half full on average), whose figures are those of sweeps of all forms, 18 problems without
 // segments and 44 with (256 CUs, head_dim 128 unless said):
@@ -639,8 +671,8 @@ double own_bytes(const cart_cache_decode_desc& d, const cart_cache& c) {
 //   37.0 / 37.2; 64 of 512 behind 512 16.0 / 22.2; 16 of 16384 behind 8192 83 / 60.6; 1 of 131072 behind 2048 31.8 / 41.1; head_dim 64: 128
 //   of 2048 behind 2048 54.0 / 34.3, 32 of 1024 behind 1024 11.3 / 14.8.  The worst choices cost 8 % (4 of 16384 behind 8192: 26.3 / 28.4).
 //   With more than 16 queries a KV head shares its keys among enough of them by itself: 25.2 / 30.1, 41.0 / 59.0, 36.0 / 33.9 of 9.
-Plan plan_of(const cart_cache_decode_desc& d, const cart_cache& c, const cart_cache_segment* shared) {
-    Plan p = {}, q = {};
+CachePlan cache_decode_plan(const cart_cache_decode_desc& d, const cart_cache& c, const cart_cache_segment* shared) {
+    CachePlan p = {}, q = {};
     const long cus = device_cus();
     long steps = 0;
     for (int s = 0; s < d.n_shared; ++s) steps += steps_of(shared[s].p);
@@ -680,34 +712,6 @@ Plan plan_of(const cart_cache_decode_desc& d, const cart_cache& c, const cart_ca
     q.n_wg = q.n_shared_wg + (static_cast<long>(q.n_ranges) * c.Hkv + 3) / 4;
     return q;
 }
-// Partial results that no plan of these sizes or smaller ones exceeds (slots of Hq rows), so that a workspace for a program's largest
-// call serves its others.  Parts: cus / (n_rb Hkv) + 1 for each request at most, and n_rb >= rows / 32.
-long most_slots(const cart_cache_decode_desc& d, const cart_cache& c, const cart_cache_segment* shared) {
-    const long cus = device_cus(), B = d.B, own = steps_of(d.max_own_len);
-    long steps = 0;
-    for (int s = 0; s < d.n_shared; ++s) steps += steps_of(shared[s].p);
-    auto least = [](long x, long y) { return x < y ? x : y; };
-    const long pieces = least(((steps + own) / MIN_CUT + 1) * B, MAX_PIECES * cus / c.Hkv + B);
-    const long parts = least((steps + 3) / 4 * B, 32 * cus / d.Hq + B + 1);
-    const long ranges = own > 0 ? least(B * (own + 1), MAX_RANGES * cus / c.Hkv + 1) + B : 0;
-    return pieces > parts + ranges ? pieces : parts + ranges;
-}
-
-template <int FMT, int D, bool NT>
-void launch(const DecodeArgs& a, const Plan& p, hipStream_t st) {
-    const dim3 grid = grid_of(p.n_wg);
-    if (p.n_cuts > 0) {
-        if (a.G <= 16) cache_decode_each_kernel<FMT, D, 16, NT><<<grid, 256, 0, st>>>(a);
-        else cache_decode_each_kernel<FMT, D, 32, NT><<<grid, 256, 0, st>>>(a);
-        if (p.n_cuts == 1) return;
-    } else if (static_cast<long>(a.B) * a.G > 16) cache_decode_split_kernel<FMT, D, 32, NT><<<grid, 256, 0, st>>>(a);
-    else cache_decode_split_kernel<FMT, D, 16, NT><<<grid, 256, 0, st>>>(a);
-    const long rows = static_cast<long>(a.B) * a.Hq;
-    if (rows <= FEW_ROWS) cache_decode_join_kernel<D, 4><<<grid_of(rows), 256, 0, st>>>(a);
-    else cache_decode_join_kernel<D, 1><<<grid_of((rows + 3) / 4), 256, 0, st>>>(a);
-}
-
-}  // namespace
 
 size_t cache_decode_workspace(const cart_cache_decode_desc& d, const cart_cache& c, const cart_cache_segment* shared) {
     return static_cast<size_t>(most_slots(d, c, shared)) * d.Hq * (c.D * sizeof(float) + sizeof(Sums));
@@ -716,7 +720,7 @@ size_t cache_decode_workspace(const cart_cache_decode_desc& d, const cart_cache&
 int launch_cache_decode(const cart_cache_decode_desc& d, const cart_cache& c, float scale, const void* q,
                         const cart_cache_segment* shared, const int32_t* table, const int32_t* cu, void* o, float* lse, void* ws,
                         hipStream_t st) {
-    const Plan p = plan_of(d, c, shared);
+    const CachePlan p = cache_decode_plan(d, c, shared);
     DecodeArgs a = {};
     a.q = static_cast<const bf16_t*>(q);
     a.k = static_cast<const char*>(c.k); a.v = static_cast<const char*>(c.v);
