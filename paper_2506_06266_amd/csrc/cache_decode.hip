@@ -278,37 +278,45 @@ struct Rows {
     }
 };
 
+// Step `local` of the n tokens that a list of blocks holds; null: no step.
+struct Where { const int32_t* list; int local, n; };
+// step s of the shared segments, one after the other
+__device__ __forceinline__ Where in_segments(const DecodeArgs& a, int s) {
+    Where w = {a.seg[0], s, a.seg_p[0]};
+    for (int k = 1; k < a.n_seg; ++k)               // (selected, not indexed: the arguments stay in scalar registers)
+        if (s >= a.seg_s0[k]) w = Where{a.seg[k], s - a.seg_s0[k], a.seg_p[k]};
+    return w;
+}
+// step `local` of request b's n own tokens
+__device__ __forceinline__ Where in_request(const DecodeArgs& a, int b, int local, int n) {
+    return Where{local >= 0 && local * STEP < n ? a.table + static_cast<size_t>(b) * a.max_blocks : nullptr, local, n};
+}
 // Up to 64 steps in the order they are taken, one a lane, as far worked out as a lane can: what a wavefront does for a step by itself
 // (reads of a lane, scalar arithmetic) is not hidden by anything of its own.
 struct Steps {
     int rows = 0;                       // keys that exist; 0: there is no such step, -1: its block is none of the pool
     uint32_t at_lo = 0, at_hi = 0;      // where its rows begin in either array of codes, bytes
     int request = 0;                    // whose, where a list has steps of several
-    float c = 0.f, lv = 0.f, unscale = 0.f;     // factors of the block: see Rows::step
+    float c = 0.f, lv = 0.f, unscale = 0.f;     // the block's scales; once settled, its factors: see Rows::step
 
-    __device__ __forceinline__ void of_block(const DecodeArgs& a, int hk, int D, int block, int local, int n_keys) {
+    __device__ __forceinline__ void put(const DecodeArgs& a, int hk, int D, const Where& w) {
+        if (!w.list) return;
         rows = -1;
+        const int block = w.list[w.local >> 1];
         if (block < 0 || block >= a.n_blocks) return;
-        rows = min(STEP, n_keys - local * STEP);
-        const size_t at = static_cast<size_t>(block) * a.Hkv + hk, from = at * (BLOCK * D) + (local & 1) * (STEP * D);
+        rows = min(STEP, w.n - w.local * STEP);
+        const size_t at = static_cast<size_t>(block) * a.Hkv + hk, from = at * (BLOCK * D) + (w.local & 1) * (STEP * D);
         at_lo = static_cast<uint32_t>(from);
         at_hi = static_cast<uint32_t>(from >> 32);
-        c = a.c * a.k_scale[at];
+        c = a.k_scale[at];
+        lv = a.v_scale[at];
+    }
+    // (after the first codes are requested, which do not wait for the scales)
+    __device__ __forceinline__ void settle(const DecodeArgs& a) {
+        c *= a.c;
         c = c < FLT_MIN ? FLT_MIN : c;  // (not 0, by which the -inf of a key that does not exist would become NaN)
-        lv = fast_log2(a.v_scale[at]);
+        lv = fast_log2(lv);
         unscale = fast_exp2(-lv);
-    }
-    // step s of the shared segments, one after the other
-    __device__ __forceinline__ void of_segments(const DecodeArgs& a, int hk, int D, int s) {
-        int i = 0;
-        for (int k = 1; k < a.n_seg; ++k) i = s >= a.seg_s0[k] ? k : i;
-        const int local = s - a.seg_s0[i];
-        of_block(a, hk, D, a.seg[i][local >> 1], local, a.seg_p[i]);
-    }
-    // step `local` of request b's n own tokens
-    __device__ __forceinline__ void of_request(const DecodeArgs& a, int hk, int D, int b, int local, int n) {
-        request = b;
-        if (local >= 0 && local * STEP < n) of_block(a, hk, D, a.table[static_cast<size_t>(b) * a.max_blocks + (local >> 1)], local, n);
     }
 };
 __device__ __forceinline__ float lane_of(float x, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i)); }
@@ -319,7 +327,7 @@ __device__ __forceinline__ int own_len(const DecodeArgs& a, int c0, int c1) { re
 
 // Takes steps 0 .. n-1 of the list, DEPTH of them in flight.  begin(request) is called ahead of each step.
 template <bool NT, int DEPTH, int FMT, int D, int Q, typename F>
-__device__ __forceinline__ void run(const DecodeArgs& a, const Steps& st, int n, int hk, Rows<FMT, D, Q>& rows, Keys<D>& keys, int lane, F&& begin) {
+__device__ __forceinline__ void run(const DecodeArgs& a, Steps& st, int n, int hk, Rows<FMT, D, Q>& rows, Keys<D>& keys, int lane, F&& begin) {
     Codes<D, Q> x[DEPTH];
     auto load = [&](Codes<D, Q>& y, int i) __attribute__((always_inline)) {
         const int at = min(i, n - 1), rows = i < n ? max(lane_of(st.rows, at), 0) : 0;
@@ -328,6 +336,7 @@ __device__ __forceinline__ void run(const DecodeArgs& a, const Steps& st, int n,
     };
 #pragma unroll
     for (int j = 0; j < DEPTH; ++j) load(x[j], j);
+    st.settle(a);
     for (int i = 0; i < n; i += DEPTH) {
 #pragma unroll
         for (int j = 0; j < DEPTH; ++j) {
@@ -419,8 +428,9 @@ __global__ __launch_bounds__(256, Q == 16 ? 3 : 1) void cache_decode_each_kernel
     for (int s = s0 + n * wv / 4; s < w1; s += 64) {
         Steps st;
         if (s + lane < w1) {
-            if (s + lane < n_shared) st.of_segments(a, hk, D, s + lane);
-            else st.of_request(a, hk, D, static_cast<int>(b), s + lane - n_shared, n_own);
+            Where w = in_segments(a, s + lane);
+            if (s + lane >= n_shared) w = in_request(a, static_cast<int>(b), s + lane - n_shared, n_own);
+            st.put(a, hk, D, w);
         }
         run<NT, 2>(a, st, min(64, w1 - s), hk, rows, lds.keys[wv], lane, [](int) {});
     }
@@ -445,10 +455,8 @@ __global__ __launch_bounds__(256, Q == 16 ? 3 : 1) void cache_decode_each_kernel
 //           requests' lengths.  (A wavefront for each request, 128 requests of 1 .. 1024 tokens: the launch waits for the longest.)
 // Partial results: part i of the segments in slot i; of range r for request b in slot n_parts B + r + b, so that neighbours never share
 // one.  Two workgroups share a CU, so that the matrix products on the segments and the streaming of the requests' own blocks overlap.
-__device__ __forceinline__ int range_len(const DecodeArgs& a) {
-    const int places = (offset_at(a.cu, a.B, INT_MAX) >> 5) + a.B;
-    return (places + a.n_ranges - 1) / a.n_ranges;
-}
+__device__ __forceinline__ int places_of(const DecodeArgs& a, int total) { return (total >> 5) + a.B; }
+__device__ __forceinline__ int range_len(const DecodeArgs& a, int places) { return (places + a.n_ranges - 1) / a.n_ranges; }
 template <int FMT, int D, int QS, bool NT>
 __global__ __launch_bounds__(256, 2) void cache_decode_split_kernel(const DecodeArgs a) {
     constexpr int QO = 16;                              // (at most 16 queries a KV head: see cache_decode_plan)
@@ -471,7 +479,7 @@ __global__ __launch_bounds__(256, 2) void cache_decode_split_kernel(const Decode
         const int p0 = static_cast<int>(total * part / a.n_parts), n = static_cast<int>(total * (part + 1) / a.n_parts) - p0, w1 = p0 + n * (wv + 1) / 4;
         for (int s = p0 + n * wv / 4; s < w1; s += 64) {
             Steps st;
-            if (s + lane < w1) st.of_segments(a, hk, D, s + lane);
+            if (s + lane < w1) st.put(a, hk, D, in_segments(a, s + lane));
             run<false, 2>(a, st, min(64, w1 - s), hk, rows, lds.keys[wv], lane, [](int) {});
         }
         __syncthreads();                                // (the keys' place)
@@ -491,7 +499,10 @@ __global__ __launch_bounds__(256, 2) void cache_decode_split_kernel(const Decode
     const int hk = static_cast<int>(w % a.Hkv);
     const long range = w / a.Hkv;
     if (range >= a.n_ranges) return;
-    const int len = range_len(a), places = (offset_at(a.cu, a.B, INT_MAX) >> 5) + a.B;
+    // fewer than 64 requests: one trip to memory for all offsets
+    const bool few = a.B < 64;
+    const int cu_lane = offset_at(a.cu, few ? min(lane, a.B) : a.B, INT_MAX);
+    const int places = places_of(a, lane_of(cu_lane, few ? a.B : 0)), len = range_len(a, places);
     const long from = range * len;
     if (from >= places) return;
     const int to = static_cast<int>(min(from + len, static_cast<long>(places)));
@@ -508,9 +519,20 @@ __global__ __launch_bounds__(256, 2) void cache_decode_split_kernel(const Decode
         });
     };
     for (int p = static_cast<int>(from); p < to; p += 64) {
-        const int n = min(64, to - p), b0 = request_of(a.cu, nullptr, a.B, INT_MAX, 5, 1, p, lane).b;
+        const int n = min(64, to - p);
         // the requests of these places: lane k looks at b0 + k, and a lane's place belongs to the last one that begins there or before
-        const int bk = min(b0 + lane, a.B - 1), c0 = offset_at(a.cu, bk, INT_MAX), c1 = offset_at(a.cu, bk + 1, INT_MAX);
+        int b0, bk, c0, c1;
+        if (few) {
+            b0 = max(static_cast<int>(__builtin_popcountll(__ballot(lane < a.B && (cu_lane >> 5) + lane <= p))) - 1, 0);
+            bk = min(b0 + lane, a.B - 1);
+            c0 = __shfl(cu_lane, bk);
+            c1 = __shfl(cu_lane, bk + 1);
+        } else {
+            b0 = request_of(a.cu, nullptr, a.B, INT_MAX, 5, 1, p, lane).b;
+            bk = min(b0 + lane, a.B - 1);
+            c0 = offset_at(a.cu, bk, INT_MAX);
+            c1 = offset_at(a.cu, bk + 1, INT_MAX);
+        }
         const long start = static_cast<long>(c0 >> 5) + bk - p;
         uint64_t begins = lane > 0 && b0 + lane < a.B && start > 0 && start < 64 ? 1ull << start : 0;
 #pragma unroll
@@ -521,7 +543,8 @@ __global__ __launch_bounds__(256, 2) void cache_decode_split_kernel(const Decode
         const int k = __builtin_popcountll(begins & ((2ull << lane) - 1));
         const int r0 = __shfl(c0, k), r1 = __shfl(c1, k), b = b0 + k;
         Steps st;
-        if (lane < n) st.of_request(a, hk, D, b, p + lane - (r0 >> 5) - b, own_len(a, r0, r1));
+        st.request = b;
+        if (lane < n) st.put(a, hk, D, in_request(a, b, p + lane - (r0 >> 5) - b, own_len(a, r0, r1)));
         run<NT, 2>(a, st, n, hk, rows, lds.keys[wv], lane, [&](int at) __attribute__((always_inline)) {
             const int request = lane_of(st.request, at);
             if (request == current) return;
@@ -557,7 +580,7 @@ __global__ __launch_bounds__(256) void cache_decode_join_kernel(const DecodeArgs
     long own = 0;
     const int c0 = a.max_own > 0 ? offset_at(a.cu, b, INT_MAX) : 0, steps = a.max_own > 0 ? steps_of(own_len(a, c0, a.cu[b + 1])) : 0;
     if (a.n_ranges > 0 && steps > 0) {
-        const int len = range_len(a), p0 = (c0 >> 5) + b, r0 = min(p0 / len, a.n_ranges - 1);
+        const int len = range_len(a, places_of(a, offset_at(a.cu, a.B, INT_MAX))), p0 = (c0 >> 5) + b, r0 = min(p0 / len, a.n_ranges - 1);
         n_own = min((p0 + steps - 1) / len, a.n_ranges - 1) - r0 + 1;
         own = static_cast<long>(n_parts) * a.B + r0 + b;
     } else if (a.n_cuts > 0) {
