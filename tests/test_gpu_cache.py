@@ -416,6 +416,16 @@ def test_long_segments_by_their_own(B, P, D, fmt):
     check_decode(*cb.cart_cache_decode(q.cuda(), c.gpu, [(i32(b), p) for b, p in many], i32(wide), i32(offsets(lens)), 64 * wide.shape[1]), ref, D)
 
 
+@pytest.mark.parametrize("B,P,Hq,Hkv", [(63, 4000, 16, 8), (64, 4000, 16, 8), (65, 4000, 16, 8), (130, 2500, 8, 4), (4100, 1500, 4, 1)])
+def test_ranges_over_many_requests(B, P, Hq, Hkv):
+    """Where a range begins is found in one, two or three trips; requests without tokens at either end and in between."""
+    lens = [0, 0] + [(37 * i) % 71 * (i % 5 > 0) for i in range(B - 4)] + [0, 0]
+    c, table, shared = filled(lens, [640], Hkv, 64, "e4m3", seed=B)
+    many = [(np.tile(shared[0][0], -(-P // 640)), P)]
+    q = rand(B, Hq, 64, seed=81, spread=0.5).bfloat16()
+    check_decode(*run_decode(c, q, many, table, lens), c.decode_ref(q, many, table, lens), 64)
+
+
 def test_blocks_past_four_gigabytes():
     """Codes whose offset passes 2^32 bytes; the scales' offsets do not."""
     Hkv, D, n_blocks = 8, 128, 70000
