@@ -272,6 +272,41 @@ def test_tokens_without_a_block(fmt):
         check_decode(*got, c.decode_ref(q, shared, nowhere, [n, n]), D)
 
 
+@pytest.mark.parametrize("fmt", FMT)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_large_calls_are_their_requests_calls(D, dtype, fmt):
+    """More than 100 MB of rows in one call, and a few requests at a time: the same codes, scales and rows."""
+    Hkv, B = 8, 30
+    T = 110000000 // (2 * Hkv * D * dtype.itemsize)
+    cuts = sorted(np.random.RandomState(D).randint(0, T, B - 1).tolist())
+    cu = [0] + cuts + [T]
+    lens = [b - a for a, b in zip(cu, cu[1:])]
+    first = [(13 * i) % 100 for i in range(B)]
+    table, n_blocks = layout(first, lens, seed=D)
+    g = torch.Generator(device="cuda").manual_seed(D)
+    x, y = (torch.randn(T, Hkv, D, generator=g, device="cuda").mul_(torch.exp2(2 * torch.randn(T, Hkv, 1, generator=g, device="cuda"))).to(dtype) for _ in range(2))
+    caches = []
+    for per in (B, 7):
+        c = cb.cache_empty(n_blocks, Hkv, D, TYPES[fmt])
+        for t in c[:2]:
+            t.view(torch.uint8).zero_()
+        for t in c[2:]:
+            t.fill_(2.0 ** -64)
+        out = [torch.empty_like(x), torch.empty_like(y)]
+        for i in range(0, B, per):
+            j = min(i + per, B)
+            rows, where = slice(cu[i], cu[j]), dict(first=i32(first[i:j]), cu_rows=i32(np.array(cu[i:j + 1]) - cu[i]))
+            cb.cart_cache_write(c, x[rows], y[rows], i32(table[i:j]), **where)
+            cb.cart_cache_read(c, out[0][rows], out[1][rows], i32(table[i:j]), **where)
+        caches.append((*[t.view(torch.uint8) for t in c], *out))
+    for a, b in zip(*caches):
+        assert torch.equal(a, b)
+    # and they are the rows that went in: half a step is 2^-4 of a value (e4m3) or half a scale (i8), which is at most twice the largest / 127
+    for z, back in zip((x, y), caches[0][4:]):
+        assert ((back.float() - z.float()).abs() <= 2.0 ** -4 * z.float().abs() + z.float().abs().max() / 127).all()
+
+
 # ---- decode -------------------------------------------------------------------------------------
 def filled(lens, seg_p, Hkv, D, fmt, seed=0, k_std=1.0):
     """A cache with the requests' tokens and the segments' in it."""
