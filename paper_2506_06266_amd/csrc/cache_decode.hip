@@ -414,9 +414,10 @@ __global__ __launch_bounds__(256, Q == 16 ? 3 : 1) void cache_decode_each_kernel
     const int lane = threadIdx.x & 63;
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const long id = static_cast<long>(blockIdx.x) + static_cast<long>(blockIdx.y) * GRID_X;
-    const int hk = static_cast<int>(id % a.Hkv), piece = static_cast<int>(id / a.Hkv % a.n_cuts);
-    const long b = id / a.Hkv / a.n_cuts;
-    if (b >= a.B) return;
+    // (the first pieces of all first: every sequence has those, so the last ones to start are short or empty)
+    const int hk = static_cast<int>(id % a.Hkv), piece = static_cast<int>(id / a.Hkv / a.B);
+    const long b = id / a.Hkv % a.B;
+    if (piece >= a.n_cuts) return;
     const int n_own = a.max_own > 0 ? own_len(a, a.cu[b], a.cu[b + 1]) : 0, n_shared = a.seg_s0[a.n_seg];
     const int s0 = piece * a.cut, s1 = min(s0 + a.cut, n_shared + steps_of(n_own));
     if (s0 >= s1 && a.n_cuts > 1) return;               // (nothing there: the join does not ask for it)
@@ -648,7 +649,7 @@ __global__ __launch_bounds__(256) void cache_decode_join_kernel(const DecodeArgs
 
 constexpr int MIN_CUT = 4;              // fewest steps of a piece: one a wavefront
 // most workgroups of pieces, and wavefronts of ranges, per CU
-constexpr int MAX_PIECES = 16, MAX_RANGES = 8;
+constexpr int MAX_PIECES = 16, MAX_RANGES = 4;
 
 double own_bytes(const cart_cache_decode_desc& d, const cart_cache& c) {
     return 0.5 * static_cast<double>(d.B) * c.Hkv * steps_of(d.max_own_len) * STEP * 2 * c.D;
@@ -683,17 +684,22 @@ void launch(const DecodeArgs& a, const CachePlan& p, hipStream_t st) {
 
 }  // namespace
 
-// The faster by an estimate (us; `own` half full on average), whose figures are those of sweeps of all forms, 18 problems without
-// segments and 44 with (256 CUs, head_dim 128 unless said):
+// The faster by an estimate (us; `own` half full on average), whose figures are those of sweeps of all forms, 40 problems without
+// segments and 300 with (256 CUs, head_dim 128 unless said):
 //   every (request, KV head) by itself, in n pieces: 5.3 and 0.14 a step of the longest piece (its four wavefronts share it) where the chip
 //     is not full, 0.6 a segment's step and SIMD -- every request's again -- and the own bytes at 6.2 TB/s; the second launch 3 and its
-//     partial results.  32 requests of up to 1024 tokens: n = 1 10.9, 2 15.3, 4 17.8; one of 16384: n = 1 76, 4 26.8, 16 14.1, 32 13.6;
-//   split: 13, the second launch's rows, and the longer of a segment wavefront's 0.73 a step and the own bytes, with some of the other; as
-//     many parts as give each CU one workgroup (128 requests of up to 1024 tokens, 8192 slots: 1 part 70, 2 53.3, 3 56.8, 4 68.9).
-//   By itself / split: 128 requests of up to 1024 tokens behind 8192 slots 146 / 48.6, of 512 behind 1024 36.4 / 26.5, of 1024 behind 512
-//   37.0 / 37.2; 64 of 512 behind 512 16.0 / 22.2; 16 of 16384 behind 8192 83 / 60.6; 1 of 131072 behind 2048 31.8 / 41.1; head_dim 64: 128
-//   of 2048 behind 2048 54.0 / 34.3, 32 of 1024 behind 1024 11.3 / 14.8.  The worst choices cost 8 % (4 of 16384 behind 8192: 26.3 / 28.4).
-//   With more than 16 queries a KV head shares its keys among enough of them by itself: 25.2 / 30.1, 41.0 / 59.0, 36.0 / 33.9 of 9.
+//     partial results.  CUs share the memory's rate evenly, so a CU with one workgroup more than others holds the call up for as
+//     long: 144 (request, head) pairs of 32000 .. 61000 tokens n = 1 336, 2 304, 4 302, 6 260, 12 265.  32 requests of up to 1024: n = 1
+//     10.9, 2 15.3, 4 17.8; one of 16384: n = 1 76, 4 26.8, 16 14.1, 32 13.6;
+//   split: 13, the second launch's rows, and the longer of a segment wavefront's 0.73 a step and the own bytes, with some of the other.  For
+//     the same reason each CU gets one workgroup of ranges, and one of the segments at most where the own bytes take longer (230
+//     requests of up to 2300 tokens behind 2268 slots: 130; with a part more, 464 workgroups of the segments, 264); where the
+//     segments take longer the CUs left over are worth another part (221 of 5 behind 5497: 45, without 52).
+//   By itself / split: 128 requests of up to 1024 tokens behind 8192 slots 164 / 48, of 512 behind 1024 36.4 / 26.5, of 1024 behind 512
+//   37.0 / 37.2; 64 of 512 behind 512 16.0 / 22.2; 16 of 16384 behind 8192 79 / 60; 1 of 131072 behind 2048 31.8 / 41.1; head_dim 64: 128
+//   of 2048 behind 2048 54.0 / 34.3, 32 of 1024 behind 1024 11.3 / 14.8.  Over 260 problems drawn like servers' the choice costs 0.7 % on
+//   average and 15 % at most.  With more than 16 queries a KV head shares its keys among enough of them by itself: 25.2 / 30.1, 41.0 /
+//   59.0, 36.0 / 33.9 of 9.
 CachePlan cache_decode_plan(const cart_cache_decode_desc& d, const cart_cache& c, const cart_cache_segment* shared) {
     CachePlan p = {}, q = {};
     const long cus = device_cus();
@@ -704,10 +710,11 @@ CachePlan cache_decode_plan(const cart_cache_decode_desc& d, const cart_cache& c
     const double chip = static_cast<double>(cus) / 256, own_us = own_bytes(d, c) / 6.2e6 / chip;
 
     double each_us = 0;
-    for (long n = 1; n == 1 || (n * MIN_CUT <= all && n * pairs <= MAX_PIECES * cus); n *= 2) {
-        const double full = static_cast<double>(pairs * n) / static_cast<double>(6 * cus);
+    // 1, 2, 3, 4, 6, 8, 12, 16 ..
+    for (long n = 1; n == 1 || (n * MIN_CUT <= all && n * pairs <= MAX_PIECES * cus); n = n == 1 ? 2 : n & (n - 1) ? n / 3 * 4 : n / 2 * 3) {
+        const double per_cu = static_cast<double>(pairs * n) / static_cast<double>(cus), full = per_cu / 6;
         const double us = 5.3 + fmax(0.14 * static_cast<double>((all + n - 1) / n) * fmax(1.0, full),
-                                     0.6 * static_cast<double>(pairs * steps) / static_cast<double>(4 * cus) + own_us) +
+                                     (0.6 * static_cast<double>(pairs * steps) / static_cast<double>(4 * cus) + own_us) * (per_cu > 1 ? ceil(per_cu) / per_cu : 1.0)) +
                           (n > 1 ? 3 + static_cast<double>(out * n) / 1000 : 0.0);
         if (n > 1 && us >= each_us) continue;
         each_us = us;
@@ -720,15 +727,19 @@ CachePlan cache_decode_plan(const cart_cache_decode_desc& d, const cart_cache& c
 
     const int per = rows > 16 ? 32 : 16;
     q.n_rb = static_cast<int>((rows + per - 1) / per);
-    const long one = static_cast<long>(q.n_rb) * c.Hkv, want = (cus + one - 1) / one, most = (steps + 3) / 4;
+    const long one = static_cast<long>(q.n_rb) * c.Hkv, most = (steps + 3) / 4;
+    auto shared_us_of = [&](long parts) { return 0.73 * static_cast<double>(steps) / (4.0 * static_cast<double>(parts)); };
+    long want = one < cus ? cus / one : 1;
+    if (cus % one != 0 && one < cus && shared_us_of(want) > own_us) ++want;
     q.n_parts = static_cast<int>(want < most ? want : most);
-    const double shared_us = 0.73 * static_cast<double>(steps) / (4.0 * q.n_parts);
+    const double shared_us = shared_us_of(q.n_parts);
     const double split_us = 13 + static_cast<double>(out) / 1200 + fmax(shared_us, own_us) + 0.3 * fmin(shared_us, own_us);
     if (each_us <= split_us) return p;
     q.n_shared_wg = one * q.n_parts;
     q.slots = static_cast<long>(q.n_parts) * d.B;
     if (own > 0) {
-        const long room = 2 * cus - q.n_shared_wg, waves = 4 * (room > cus / 2 ? room : cus / 2), places = static_cast<long>(d.B) * (own + 1), r = waves / c.Hkv;
+        const long room = 2 * cus - q.n_shared_wg, wgs = room > cus ? cus : room > cus / 2 ? room : cus / 2;
+        const long r = 4 * wgs / c.Hkv, places = static_cast<long>(d.B) * (own + 1);
         q.n_ranges = static_cast<int>(r < 1 ? 1 : r < places ? r : places);
         q.slots += q.n_ranges + d.B;
     }
